@@ -293,6 +293,78 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
                              void *Y, sq_dtype y_dtype, int64_t ldy, void *acc_dump,
                              void *workspace, size_t ws_bytes, void *stream);
 
+/* 4-bit weights with one scale, and optionally one zero-point, per output channel n and group g = k / group of inputs (finer
+ * than the per-channel scales of the W4A8 calls above; weights only, activations stay real numbers), and the product of
+ * few rows of activations with them: the modulation projections of a block (one conditioning vector per sample), single tokens.
+ *       w'[n][k] = (c[n][k] - z[g][n]) * s[g][n]
+ *   segquant_quantize_w4_group (offline), per (n, g), one IEEE fp32 division each, round half to even:
+ *     z_w == NULL (symmetric): s = max|w| / 7,  c = clip(round(w / s), -7, 7);
+ *     z_w != NULL (App. A):    lo = min(min w, 0), hi = max(max w, 0), s = (hi - lo) / 15, z = -8 - round(lo / s),
+ *                              c = clip(round(w / s) + z, -8, 7).
+ *     s is rounded to s_dtype before it is used (1 where that gives 0).  W [N,K] dev (dtype dt, ld elements), finite, its
+ *     extrema below 2^127 in magnitude.
+ *   Layout: Wq4 [N] rows of (K + 1) / 2 bytes, pitch ldw bytes, code 2j in the low nibble of byte j (as segquant_pack_w4), the
+ *     last high nibble 0 for odd K; s_w [groups][N] of s_dtype (fp32 or bf16), pitch lds elements; z_w [groups][N] int8, pitch
+ *     ldz; groups = ceil(K / group), the last one may be short.  group: 32, 64, 128 or a multiple of 256.
+ *   segquant_dequantize_w4_group: W [N,K] of dtype dt from them, one fp32 product each, rounded once to dt.
+ *   segquant_w4_matvec: y[m][n] = sum_g s[g][n] * ( sum_{k in g} (c[n][k] - z[g][n]) * a[m][k] ) + bias[n],
+ *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused; NOT rounded
+ *     to dt in between).  Products are exact, a group's sum and the sum over groups are fp32 in an order that depends on the
+ *     sizes and the device alone; one rounding to y_dtype.  X [M,K] dev (dtype dt, ldx elements), bias dev [N] fp32 or NULL, Y [M,N]
+ *     dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements only; Y must not overlap X.  Codes of
+ *     any 4 bits, zero-points in [-120, 120].  K <= 131072; any M, meant for M of at most about 32 (the weights are read once
+ *     per pass of up to 32 bf16 rows; 10 rows where x is fp32 or behind an activation function).  No workspace.
+ *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
+ *     N <= 2097120 for the two offline calls. */
+sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *Wq4,
+                                     int64_t ldw, void *s_w, sq_dtype s_dtype, int64_t lds, int8_t *z_w, int64_t ldz, void *stream);
+sq_status segquant_dequantize_w4_group(const void *Wq4, int64_t ldw, int64_t N, int64_t K, int64_t group, const void *s_w,
+                                       sq_dtype s_dtype, int64_t lds, const int8_t *z_w, int64_t ldz, void *W, sq_dtype dt,
+                                       int64_t ld, void *stream);
+sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, int64_t ldx, sq_act act, const void *Wq4, int64_t ldw,
+                             int64_t N, int64_t group, const void *s_w, sq_dtype s_dtype, int64_t lds, const int8_t *z_w,
+                             int64_t ldz, const float *bias, void *Y, sq_dtype y_dtype, int64_t ldy, void *stream);
+
+/* The end of one block and the start of the next, in one pass over the rows: gate, residual and norms around the quantized
+ * layers.  Per row m of sample b = m / rows_per_sample, over its C channels:
+ *       u = post(y) * post_w + post_b                              (post: none, RMS norm or layer norm of the block's output y)
+ *       h = r + alpha * gate[b] * u                                (r: residual stream)
+ *       o = pre(h) * w + b;   o = o * (1 + scale[b]) + shift[b]    (pre: the next block's norm)
+ *   RMS norm: x / sqrt(mean(x^2) + eps); layer norm: (x - mean) / sqrt(mean((x - mean)^2) + eps).  Every vector may be NULL
+ *   (left out).  R == NULL: r = 0.  Y == NULL: h = r, and post, gate and their vectors must be left out as well.
+ *   All in fp32; h is stored rounded to dt, the norm behind it sees the unrounded value.
+ *   segquant_block_norm: H [M,C] (the new residual stream; NULL: not stored) and O [M,C] (NULL: not computed), both of dtype dt.
+ *   segquant_block_norm_quantize: instead of O the codes that segquant_quantize_act defines for it (segment table over C, s_pos,
+ *     s_neg, code and flags as there), o entering the quantizer unrounded: the norm in front of a SegLinear / DualScale layer
+ *     without its output in device memory.  The quotient o / s carries the fp32 error of o, so a code may be the neighbouring one
+ *     where the exact quotient lies that close to a rounding boundary.
+ *   Y, R, H, O dev, dtype dt, pitches in elements; H and O may be Y or R themselves (same address and pitch), any other overlap
+ *   is refused with SQ_ERR_UNSUPPORTED.  Alignment: Y, R, H, O and codes 16 bytes, pitches multiples of 16 bytes; the vectors
+ *   that of their elements.  C <= 16384.  Values beyond about 2^60 overflow the sums of squares. */
+typedef enum { SQ_NORM_NONE = 0, SQ_NORM_RMS = 1, SQ_NORM_LAYER = 2 } sq_norm;
+typedef struct {
+    sq_norm post;                             /* norm of the block's output */
+    const void *post_w, *post_b;              /* dev [C] */
+    float alpha;                              /* residual scale */
+    const void *gate;                         /* dev [samples][C], pitch ld_gate elements; pitch 0: one vector for all */
+    int64_t ld_gate;
+    sq_norm pre;                              /* norm in front of the next block */
+    const void *w, *b;                        /* dev [C] */
+    const void *scale;                        /* dev [samples][C] */
+    int64_t ld_scale;
+    const void *shift;                        /* dev [samples][C] */
+    int64_t ld_shift;
+    sq_dtype p_dtype;                         /* type of all vectors */
+    int64_t rows_per_sample;                  /* >= 1; the last sample may have fewer */
+    float eps;                                /* >= 0 */
+} sq_block_norm;
+sq_status segquant_block_norm(const void *Y, int64_t ldy, const void *R, int64_t ldr, sq_dtype dt, int64_t M, int64_t C,
+                              const sq_block_norm *norm, void *H, int64_t ldh, void *O, int64_t ldo, void *stream);
+sq_status segquant_block_norm_quantize(const void *Y, int64_t ldy, const void *R, int64_t ldr, sq_dtype dt, int64_t M, int64_t C,
+                                       const sq_block_norm *norm, void *H, int64_t ldh, const sq_segtable *seg,
+                                       const float *s_pos, const float *s_neg, sq_code code, uint32_t flags, void *c_pos,
+                                       void *c_neg, int64_t ldc, void *stream);
+
 /* A layer call prepared once and replayed.  segquant_plan_layer does everything segquant_layer_forward does on
  * the host for device X and Y -- argument checks, tile plan, kernel choice, tensor-map encoding, attribute set-up --
  * and stores the result in caller-owned memory instead of launching; segquant_plan_run then issues the layer's

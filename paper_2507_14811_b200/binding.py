@@ -30,7 +30,8 @@ EXPORTS = [
     "segquant_status_string", "segquant_quantize_act_fused", "segquant_calib_zero_point",
     "segquant_quantize_act_zero_point", "segquant_fold_zero_point", "segquant_plan_layer", "segquant_plan_run",
     "segquant_quantize_per_row", "segquant_pack_w4", "segquant_unpack_w4", "segquant_w4a8_gemm",
-    "segquant_split_workspace_bytes", "segquant_set_quantize_tuning",
+    "segquant_split_workspace_bytes", "segquant_set_quantize_tuning", "segquant_quantize_w4_group",
+    "segquant_dequantize_w4_group", "segquant_w4_matvec", "segquant_block_norm", "segquant_block_norm_quantize",
 ]
 
 
@@ -355,6 +356,73 @@ def segquant_w4a8_gemm(Xq_pos, Xq_neg, Wq8, seg: SegTable, s_pos, s_neg, s_w, bi
     st = _calls().gemm(Xq_pos, Xq_neg, Wq8, seg.address, SQ_CODE["int8"], s_pos, s_neg, s_w, bias, Y, dump, workspace, _W4A8)
     _check(st, "segquant_w4a8_gemm")
     return (Y, dump) if dump_acc else Y
+
+
+_REAL = {torch.float32: SQ_F32, torch.bfloat16: SQ_BF16}
+
+
+def _real(dtype) -> int:
+    if dtype not in _REAL:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _REAL[dtype]
+
+
+def _named(table, name, what) -> int:
+    if name not in table:
+        raise ValueError(f"unknown {what} {name!r}")
+    return table[name]
+
+
+def segquant_quantize_w4_group(W: torch.Tensor, group: int, s_dtype=torch.float32, zero_points: bool = False):
+    """(Wq4 [N, ceil(K / 2)], s_w [groups, N], z_w [groups, N] | None): 4-bit codes with one scale, and on request one
+    zero-point, per output channel and group of inputs.  group: 32, 64, 128 or a multiple of 256."""
+    st, Wq4, s_w, z_w = _calls().quantize_w4_group(W, group, _real(s_dtype), zero_points)
+    _check(st, "segquant_quantize_w4_group")
+    return Wq4, s_w, z_w
+
+
+def segquant_dequantize_w4_group(Wq4: torch.Tensor, s_w, group: int, K: int, z_w=None, dtype=torch.bfloat16, W=None):
+    """The weights [N, K] that the codes stand for."""
+    st, W = _calls().dequantize_w4_group(Wq4, s_w, group, K, z_w, W, _real(dtype))
+    _check(st, "segquant_dequantize_w4_group")
+    return W
+
+
+_W4_ACT = {None: 0, "none": 0, "silu": 1, "gelu": 2}
+
+
+def segquant_w4_matvec(X: torch.Tensor, Wq4, s_w, group: int, z_w=None, bias=None, act=None, y_dtype=torch.bfloat16, Y=None):
+    """Few rows X [M, K] times the transpose of 4-bit weights with group scales, the activation function in front and the
+    bias behind: Y [M, N].  Weights as segquant_quantize_w4_group makes them."""
+    st, Y = _calls().w4_matvec(X, Wq4, s_w, group, z_w, bias, _named(_W4_ACT, act, "activation"), Y, _real(y_dtype))
+    _check(st, "segquant_w4_matvec")
+    return Y
+
+
+SQ_NORM = {None: 0, "none": 0, "rms": 1, "layer": 2}
+
+
+def segquant_block_norm(R, Y=None, gate=None, alpha: float = 1.0, post=None, post_w=None, post_b=None, norm="layer", w=None, b=None,
+                        scale=None, shift=None, rows_per_sample=None, eps: float = 1e-6, H=None, out=None, store_out: bool = True):
+    """End of one block and start of the next: H = R + alpha gate post(Y), out = norm(H) w + b, times 1 + scale, plus shift.
+    R, Y, H, out [M, C]; gate, scale, shift [samples, C] (or [C]) with rows_per_sample rows each (default: all); w, b, post_w,
+    post_b [C].  Returns (H, out); H is R itself where there is no Y, out None with store_out=False.  H and out may be given,
+    R or Y themselves among them."""
+    st, H, out = _calls().block_norm(R, Y, _named(SQ_NORM, post, "norm"), post_w, post_b, alpha, gate, _named(SQ_NORM, norm, "norm"), w, b,
+                                     scale, shift, rows_per_sample, eps, H, out, store_out)
+    _check(st, "segquant_block_norm")
+    return H, out
+
+
+def segquant_block_norm_quantize(R, seg: SegTable, s_pos, s_neg, code: str, Y=None, gate=None, alpha: float = 1.0, post=None, post_w=None,
+                                 post_b=None, norm="layer", w=None, b=None, scale=None, shift=None, rows_per_sample=None,
+                                 eps: float = 1e-6, H=None, flags: int = 0, c_pos=None, c_neg=None):
+    """segquant_block_norm with the codes of the layer behind it in the place of out: (H, c_pos, c_neg | None)."""
+    st, H, c_pos, c_neg = _calls().block_norm_quantize(
+        R, Y, _named(SQ_NORM, post, "norm"), post_w, post_b, alpha, gate, _named(SQ_NORM, norm, "norm"), w, b, scale, shift, rows_per_sample,
+        eps, H, seg.address, seg.P, s_pos, s_neg, SQ_CODE[code], flags, c_pos, c_neg)
+    _check(st, "segquant_block_norm_quantize")
+    return H, c_pos, c_neg
 
 
 SQ_PLAN_BYTES = 4096

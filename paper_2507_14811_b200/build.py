@@ -13,9 +13,10 @@ INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libsegquant.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 # (source, object, defines): the GEMM's kernel instantiations are spread over four units that compile side by side
-UNITS = [(f, f.replace(".cu", ".o"), []) for f in ("api.cu", "calib.cu", "quantize.cu", "zero_point.cu", "gemm_tcgen05.cu")]
+UNITS = [(f, f.replace(".cu", ".o"), []) for f in ("api.cu", "calib.cu", "quantize.cu", "zero_point.cu", "w4_group.cu", "block_norm.cu", "gemm_tcgen05.cu")]
 UNITS += [("gemm_tcgen05.cu", f"gemm_kind{k}_npol{n}.o", [f"-DSQ_GEMM_KIND={k}", f"-DSQ_GEMM_NPOL={n}"])
           for k in (0, 1) for n in (1, 2)]
+UNITS += [("block_norm.cu", f"block_norm_out{o}.o", [f"-DSQ_NORM_OUT={o}"]) for o in range(5)]      # one kind of output each
 CALLS_PATH = os.path.join(_HERE, "_calls.so")          # native module over the library, for torch tensors
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]

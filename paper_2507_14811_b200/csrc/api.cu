@@ -143,6 +143,84 @@ static bool fused_layer(const void *X, sq_dtype dt, int64_t M, int64_t K, int64_
     return prepare_fused_layer(g, L) == SQ_OK;
 }
 
+// Whether two matrices of `rows` rows, `wa` / `wb` bytes wide with pitches `pa` / `pb`, may share a byte.  Column ranges of one
+// buffer (equal pitches) that do not meet are told apart; other pitches count as overlapping wherever the extents do.
+static bool rows_overlap(const void *a, int64_t pa, int64_t wa, const void *b, int64_t pb, int64_t wb, int64_t rows)
+{
+    if (!a || !b || !overlap(a, size_t((rows - 1) * pa + wa), b, size_t((rows - 1) * pb + wb))) return false;
+    if (pa != pb || pa <= 0) return true;
+    const intptr_t d = reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a);
+    const int64_t shift = ((d % pa) + pa) % pa;          // where b's rows start within a's pitch
+    return shift < wa || shift + wb > pa;
+}
+
+// ---- 4-bit weights with group scales
+struct W4Group {
+    const void *W4;
+    int64_t ldw, N, K, group;
+    const void *s;
+    sq_dtype s_dtype;
+    int64_t lds;
+    const int8_t *z;
+    int64_t ldz;
+};
+
+static sq_status check_w4_group(const W4Group &w)
+{
+    if (!w.W4 || !w.s) return SQ_ERR_NULL;
+    if (!valid_dt(w.s_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (w.N <= 0 || w.K <= 0 || w.N > kMaxDim || w.K > kMaxDim || w.ldw < (w.K + 1) / 2 || w.lds < w.N || (w.z && w.ldz < w.N))
+        return SQ_ERR_SHAPE;
+    if (w.group != 32 && w.group != 64 && w.group != 128 && (w.group <= 0 || w.group % 256 != 0)) return SQ_ERR_UNSUPPORTED;
+    if (!aligned16(w.W4) || !aligned16(w.s) || w.ldw % 16 != 0 || (w.lds * int64_t(dt_size(w.s_dtype))) % 16 != 0) return SQ_ERR_ALIGN;
+    if (w.z && (!aligned16(w.z) || w.ldz % 16 != 0)) return SQ_ERR_ALIGN;
+    return SQ_OK;
+}
+
+// ---- block norms
+constexpr int64_t kMaxNormC = 16384;      // a row is held in one thread block's registers
+
+static bool valid_norm(sq_norm n) { return n == SQ_NORM_NONE || n == SQ_NORM_RMS || n == SQ_NORM_LAYER; }
+
+static sq_status check_block_norm(const BlockNormArgs &a)
+{
+    const sq_block_norm *n = a.norm;
+    if (!n || (!a.Y && !a.R)) return SQ_ERR_NULL;
+    if (!valid_dt(a.dt) || !valid_dt(n->p_dtype) || !valid_norm(n->post) || !valid_norm(n->pre)) return SQ_ERR_UNSUPPORTED;
+    if (!a.Y && (n->post != SQ_NORM_NONE || n->post_w || n->post_b || n->gate)) return SQ_ERR_NULL;
+    const size_t size = dt_size(a.dt);
+    sq_status st;
+    if (a.Y && (st = check_matrix(a.Y, a.M, a.C, a.ldy, size)) != SQ_OK) return st;
+    if (a.R && (st = check_matrix(a.R, a.M, a.C, a.ldr, size)) != SQ_OK) return st;
+    if (a.H && (st = check_matrix(a.H, a.M, a.C, a.ldh, size)) != SQ_OK) return st;
+    if (a.O && (st = check_matrix(a.O, a.M, a.C, a.ldo, size)) != SQ_OK) return st;
+    if (a.C > kMaxNormC) return SQ_ERR_UNSUPPORTED;
+    if (n->rows_per_sample < 1) return SQ_ERR_SHAPE;
+    if ((n->gate && n->ld_gate != 0 && n->ld_gate < a.C) || (n->scale && n->ld_scale != 0 && n->ld_scale < a.C) ||
+        (n->shift && n->ld_shift != 0 && n->ld_shift < a.C))
+        return SQ_ERR_SHAPE;
+    const uintptr_t elem = dt_size(n->p_dtype) - 1;
+    for (const void *v : {n->post_w, n->post_b, n->gate, n->w, n->b, n->scale, n->shift})
+        if (reinterpret_cast<uintptr_t>(v) & elem) return SQ_ERR_ALIGN;
+    if (!(n->eps >= 0.0f)) return SQ_ERR_UNSUPPORTED;
+    // an output may stand in the place of an input, row for row; anything else that overlaps would be read after it was written
+    const int64_t bytes = a.C * int64_t(size);
+    const struct { const void *p; int64_t pitch; } in[2] = {{a.Y, a.ldy * int64_t(size)}, {a.R, a.ldr * int64_t(size)}},
+        out[2] = {{a.H, a.ldh * int64_t(size)}, {a.O, a.ldo * int64_t(size)}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (!(o.p == i.p && o.pitch == i.pitch) && rows_overlap(o.p, o.pitch, bytes, i.p, i.pitch, bytes, a.M)) return SQ_ERR_UNSUPPORTED;
+    if (rows_overlap(a.H, out[0].pitch, bytes, a.O, out[1].pitch, bytes, a.M)) return SQ_ERR_UNSUPPORTED;
+    for (const void *c : {static_cast<const void *>(a.c_pos), static_cast<const void *>(a.c_neg)}) {
+        if (!c) continue;
+        for (const auto &i : in)
+            if (rows_overlap(c, a.ldc, a.C, i.p, i.pitch, bytes, a.M)) return SQ_ERR_UNSUPPORTED;
+        if (rows_overlap(c, a.ldc, a.C, a.H, out[0].pitch, bytes, a.M)) return SQ_ERR_UNSUPPORTED;
+    }
+    if (rows_overlap(a.c_pos, a.ldc, a.C, a.c_neg, a.ldc, a.C, a.M)) return SQ_ERR_UNSUPPORTED;
+    return SQ_OK;
+}
+
 // What an sq_plan holds (copied in and out of the caller's storage, which need not be aligned for it).
 struct LayerPlan {
     uint64_t magic;
@@ -493,6 +571,77 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
     const sq_status st = gemm_args(Xq_pos, Xq_neg, dual, ldx, Wq8, ldw, M, N, K, seg, SQ_CODE_INT8, s_pos, s_neg, s_w,
                                    bias, Y, y_dtype, ldy, acc_dump, workspace, ws_bytes, &g, 1);
     return st == SQ_OK ? launch_gemm(g, static_cast<cudaStream_t>(stream)) : st;
+}
+
+sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *Wq4,
+                                     int64_t ldw, void *s_w, sq_dtype s_dtype, int64_t lds, int8_t *z_w, int64_t ldz, void *stream)
+{
+    if (!valid_dt(dt)) return SQ_ERR_UNSUPPORTED;
+    sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
+    if (st != SQ_OK) return st;
+    if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
+    return launch_quantize_w4_group(W, dt, N, K, ld, group, Wq4, ldw, s_w, s_dtype, lds, z_w, ldz, static_cast<cudaStream_t>(stream));
+}
+
+sq_status segquant_dequantize_w4_group(const void *Wq4, int64_t ldw, int64_t N, int64_t K, int64_t group, const void *s_w,
+                                       sq_dtype s_dtype, int64_t lds, const int8_t *z_w, int64_t ldz, void *W, sq_dtype dt,
+                                       int64_t ld, void *stream)
+{
+    if (!valid_dt(dt)) return SQ_ERR_UNSUPPORTED;
+    sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
+    if (st != SQ_OK) return st;
+    if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
+    return launch_dequantize_w4_group(Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz, W, dt, ld, static_cast<cudaStream_t>(stream));
+}
+
+sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, int64_t ldx, sq_act act, const void *Wq4, int64_t ldw,
+                             int64_t N, int64_t group, const void *s_w, sq_dtype s_dtype, int64_t lds, const int8_t *z_w,
+                             int64_t ldz, const float *bias, void *Y, sq_dtype y_dtype, int64_t ldy, void *stream)
+{
+    if (!X || !Y) return SQ_ERR_NULL;
+    if (!valid_dt(dt) || !valid_dt(y_dtype)) return SQ_ERR_UNSUPPORTED;
+    if (act != SQ_ACT_NONE && act != SQ_ACT_SILU && act != SQ_ACT_GELU) return SQ_ERR_UNSUPPORTED;
+    if (M <= 0 || M > 65535 || K <= 0 || K > kMaxK || ldx < K || ldy < N) return SQ_ERR_SHAPE;
+    const sq_status st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz});
+    if (st != SQ_OK) return st;
+    const int64_t xs = int64_t(dt_size(dt)), ys = int64_t(dt_size(y_dtype));
+    if (reinterpret_cast<uintptr_t>(X) % xs || reinterpret_cast<uintptr_t>(Y) % ys || (reinterpret_cast<uintptr_t>(bias) & 3u))
+        return SQ_ERR_ALIGN;
+    if (rows_overlap(X, ldx * xs, K * xs, Y, ldy * ys, N * ys, M)) return SQ_ERR_UNSUPPORTED;
+    return launch_w4_matvec({X, dt, M, K, ldx, act, Wq4, ldw, N, group, s_w, s_dtype, lds, z_w, ldz, bias, Y, y_dtype, ldy},
+                            static_cast<cudaStream_t>(stream));
+}
+
+sq_status segquant_block_norm(const void *Y, int64_t ldy, const void *R, int64_t ldr, sq_dtype dt, int64_t M, int64_t C,
+                              const sq_block_norm *norm, void *H, int64_t ldh, void *O, int64_t ldo, void *stream)
+{
+    if (!H && !O) return SQ_ERR_NULL;
+    BlockNormArgs a{};
+    a.Y = Y; a.ldy = ldy; a.R = R; a.ldr = ldr; a.dt = dt; a.M = M; a.C = C; a.norm = norm; a.H = H; a.ldh = ldh; a.O = O; a.ldo = ldo;
+    const sq_status st = check_block_norm(a);
+    return st == SQ_OK ? launch_block_norm(a, static_cast<cudaStream_t>(stream)) : st;
+}
+
+sq_status segquant_block_norm_quantize(const void *Y, int64_t ldy, const void *R, int64_t ldr, sq_dtype dt, int64_t M, int64_t C,
+                                       const sq_block_norm *norm, void *H, int64_t ldh, const sq_segtable *seg,
+                                       const float *s_pos, const float *s_neg, sq_code code, uint32_t flags, void *c_pos,
+                                       void *c_neg, int64_t ldc, void *stream)
+{
+    if (!s_pos || !c_pos || (s_neg && !c_neg)) return SQ_ERR_NULL;
+    if (!valid_code(code)) return SQ_ERR_UNSUPPORTED;
+    BlockNormArgs a{};
+    a.Y = Y; a.ldy = ldy; a.R = R; a.ldr = ldr; a.dt = dt; a.M = M; a.C = C; a.norm = norm; a.H = H; a.ldh = ldh;
+    a.code = code; a.q_max = code_qmax(code); a.q_min_abs = code_qmin_abs(code, flags);
+    a.s_pos = s_pos; a.s_neg = s_neg;
+    a.c_pos = c_pos; a.c_neg = s_neg ? c_neg : nullptr; a.ldc = ldc;
+    sq_status st;
+    if ((st = check_matrix(c_pos, M, C, ldc, 1)) != SQ_OK) return st;
+    if (s_neg && (st = check_matrix(c_neg, M, C, ldc, 1)) != SQ_OK) return st;
+    if ((st = check_block_norm(a)) != SQ_OK) return st;
+    const HostSeg hs = load_segtable(seg, C, seg && seg->nb && seg->Q >= 1 ? seg->nb[seg->Q] : 0);
+    if (hs.status != SQ_OK) return hs.status;
+    a.sb = hs.b;
+    return launch_block_norm(a, static_cast<cudaStream_t>(stream));
 }
 
 sq_status segquant_plan_layer(sq_plan *plan, const void *X, sq_dtype dt, int64_t M, int64_t K, int64_t ld,

@@ -108,6 +108,48 @@ sq_status launch_fold_zero_point(const void *Wq, int64_t ldw, int64_t N, int64_t
                                  const float *s_x, const int32_t *z_x, const float *s_w, const float *bias,
                                  float *bias_folded, cudaStream_t st);
 
+// 4-bit weights with one scale (and zero-point) per channel and group of inputs (w4_group.cu).
+sq_status launch_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *W4, int64_t ldw,
+                                   void *s, sq_dtype s_dtype, int64_t lds, int8_t *z, int64_t ldz, cudaStream_t st);
+sq_status launch_dequantize_w4_group(const void *W4, int64_t ldw, int64_t N, int64_t K, int64_t group, const void *s, sq_dtype s_dtype,
+                                     int64_t lds, const int8_t *z, int64_t ldz, void *W, sq_dtype dt, int64_t ld, cudaStream_t st);
+struct W4MatvecArgs {
+    const void *X;
+    sq_dtype dt;
+    int64_t M, K, ldx;
+    sq_act act;
+    const void *W4;
+    int64_t ldw, N, group;
+    const void *s;
+    sq_dtype s_dtype;
+    int64_t lds;
+    const int8_t *z;
+    int64_t ldz;
+    const float *bias;
+    void *Y;
+    sq_dtype y_dtype;
+    int64_t ldy;
+};
+sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st);
+
+// End of one block and start of the next (block_norm.cu).
+struct BlockNormArgs {
+    const void *Y, *R;
+    int64_t ldy, ldr;
+    sq_dtype dt;
+    int64_t M, C;
+    const sq_block_norm *norm;
+    void *H, *O;
+    int64_t ldh, ldo;
+    SegBounds sb;                // codes instead of O: c_pos != nullptr
+    sq_code code;
+    float q_max, q_min_abs;
+    const float *s_pos, *s_neg;
+    void *c_pos, *c_neg;
+    int64_t ldc;
+};
+sq_status launch_block_norm(const BlockNormArgs &a, cudaStream_t st);
+
 struct GemmArgs {
     const void *a_pos, *a_neg;   // code matrices [M,K]; a_neg == nullptr: single path
     int64_t lda;

@@ -9,6 +9,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include "segquant.h"
 
@@ -291,6 +292,276 @@ PyObject *unpack_w4(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---- 4-bit weights with group scales and block norms: the tensors are held to what the C ABI takes of them
+
+[[noreturn]] void refuse(PyObject *type, const char *format, const char *what)
+{
+    PyErr_Format(type, format, what);
+    throw BadArgument();
+}
+
+// A CUDA tensor of the current device.
+const at::Tensor &on_device(const at::Tensor &t, const char *what)
+{
+    if (!t.is_cuda()) refuse(PyExc_ValueError, "%s must be a CUDA tensor", what);
+    if (t.get_device() != c10::cuda::current_device()) refuse(PyExc_ValueError, "%s is on another device than the current one", what);
+    return t;
+}
+
+// A matrix with consecutive columns (int64 pitch in elements); `rows` / `cols` < 0: any.
+struct Matrix {
+    void *p = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+    Matrix() = default;
+    Matrix(const at::Tensor &t, const char *what, int64_t want_rows = -1, int64_t want_cols = -1)
+    {
+        if (t.dim() != 2) refuse(PyExc_ValueError, "%s must be a matrix", what);
+        rows = t.size(0), cols = t.size(1);
+        if ((want_rows >= 0 && rows != want_rows) || (want_cols >= 0 && cols != want_cols)) refuse(PyExc_ValueError, "%s has another shape than the call's", what);
+        if (cols > 1 && t.stride(1) != 1) refuse(PyExc_ValueError, "the columns of %s must lie one behind the other", what);
+        on_device(t, what);
+        p = t.data_ptr();
+        ld = rows == 1 ? (cols + 15) / 16 * 16 : t.stride(0);        // the pitch of a single row is nobody's
+    }
+};
+
+void want_type(const at::Tensor &t, at::ScalarType type, const char *what)
+{
+    if (t.scalar_type() != type) refuse(PyExc_TypeError, "%s has the wrong dtype", what);
+}
+
+// fp32 vector of at least n elements, or None
+float *f32_vector(const Args &a, int i, int64_t n, const char *what)
+{
+    if (a.none(i)) return nullptr;
+    const at::Tensor &t = a.tensor(i);
+    want_type(t, at::kFloat, what);
+    if (t.numel() < n || !t.is_contiguous()) refuse(PyExc_ValueError, "%s is too short or not contiguous", what);
+    return static_cast<float *>(on_device(t, what).data_ptr());
+}
+
+// [rows, cols] with rows on boundaries of 16 bytes (and of 16 elements)
+at::Tensor new_rows(int64_t rows, int64_t cols, const at::Tensor &like, at::ScalarType type)
+{
+    return at::empty({rows, (cols + 15) / 16 * 16}, like.options().dtype(type)).narrow(1, 0, cols);
+}
+
+struct GroupScales {
+    Matrix s, z;
+    sq_dtype type;
+    GroupScales(const Args &a, int is, int iz, int64_t groups, int64_t N) : s(a.matrix(is), "s_w", groups, N), type(dtype_of(a.tensor(is)))
+    {
+        if (a.none(iz)) return;
+        want_type(a.tensor(iz), at::kChar, "z_w");
+        z = Matrix(a.tensor(iz), "z_w", groups, N);
+    }
+};
+
+int64_t groups_of(int64_t K, int64_t group)
+{
+    if (group <= 0) refuse(PyExc_ValueError, "%s must be positive", "group");
+    return (K + group - 1) / group;
+}
+
+at::ScalarType real_type(const Args &a, int i) { return a.integer(i) == SQ_F32 ? at::kFloat : at::kBFloat16; }
+
+// X, W4, s_w, group, z_w | None, bias | None, act, Y | None, type of a new Y -> (status, Y)
+PyObject *w4_matvec(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded("w4_matvec", n, 9, [&]() -> PyObject * {
+        const Args a{args};
+        const at::Tensor &x = a.matrix(0);
+        const sq_dtype dx = dtype_of(x);
+        want_type(a.tensor(1), at::kByte, "Wq4");
+        const Matrix X(x, "X"), W(a.matrix(1), "Wq4", -1, (X.cols + 1) / 2);
+        const int64_t group = a.integer(3);
+        const GroupScales sc(a, 2, 4, groups_of(X.cols, group), W.rows);
+        const float *bias = f32_vector(a, 5, W.rows, "bias");
+        const sq_act act = sq_act(a.integer(6));
+        const at::Tensor y = a.none(7) ? at::empty({X.rows, W.rows}, x.options().dtype(real_type(a, 8))) : a.tensor(7);
+        const sq_dtype dy = dtype_of(y);
+        const Matrix Y(y, "Y", X.rows, W.rows);
+        void *stream = current_stream();
+        const sq_status st = without_gil([&] {
+            return segquant_w4_matvec(X.p, dx, X.rows, X.cols, X.ld, act, W.p, W.ld, W.rows, group, sc.s.p, sc.type, sc.s.ld,
+                                      static_cast<const int8_t *>(sc.z.p), sc.z.ld, bias, Y.p, dy, Y.ld, stream);
+        });
+        return Py_BuildValue("(iN)", int(st), THPVariable_Wrap(y));
+    });
+}
+
+// W, group, type of the scales, zero_points -> (status, W4, s_w, z_w | None)
+PyObject *quantize_w4_group(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded("quantize_w4_group", n, 4, [&]() -> PyObject * {
+        const Args a{args};
+        const at::Tensor &w = a.matrix(0);
+        const sq_dtype dw = dtype_of(w);
+        const Matrix W(w, "W");
+        const int64_t group = a.integer(1), groups = groups_of(W.cols, group), N = W.rows;
+        const at::ScalarType ts = real_type(a, 2);
+        const bool zp = a.truth(3);
+        const at::Tensor q = new_rows(N, (W.cols + 1) / 2, w, at::kByte), s = new_rows(groups, N, w, ts);
+        const at::Tensor z = zp ? new_rows(groups, N, w, at::kChar) : at::Tensor();
+        const Rows Q(q), S(s);
+        int8_t *zp_p = zp ? static_cast<int8_t *>(z.data_ptr()) : nullptr;
+        const int64_t ldz = zp ? z.stride(0) : 0;
+        void *stream = current_stream();
+        const sq_status st = without_gil([&] {
+            return segquant_quantize_w4_group(W.p, dw, N, W.cols, W.ld, group, Q.p, Q.ld, S.p, ts == at::kFloat ? SQ_F32 : SQ_BF16, S.ld, zp_p,
+                                              ldz, stream);
+        });
+        return Py_BuildValue("(iNNN)", int(st), THPVariable_Wrap(q), THPVariable_Wrap(s), THPVariable_Wrap(z));
+    });
+}
+
+// W4, s_w, group, K, z_w | None, W | None, type of a new W -> (status, W)
+PyObject *dequantize_w4_group(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded("dequantize_w4_group", n, 7, [&]() -> PyObject * {
+        const Args a{args};
+        const at::Tensor &q = a.matrix(0);
+        want_type(q, at::kByte, "Wq4");
+        const int64_t group = a.integer(2), K = a.integer(3);
+        const Matrix Q(q, "Wq4", -1, (K + 1) / 2);
+        const GroupScales sc(a, 1, 4, groups_of(K, group), Q.rows);
+        const at::Tensor w = a.none(5) ? new_rows(Q.rows, K, q, real_type(a, 6)) : a.tensor(5);
+        const sq_dtype dw = dtype_of(w);
+        const Matrix W(w, "W", Q.rows, K);
+        void *stream = current_stream();
+        const sq_status st = without_gil([&] {
+            return segquant_dequantize_w4_group(Q.p, Q.ld, Q.rows, K, group, sc.s.p, sc.type, sc.s.ld, static_cast<const int8_t *>(sc.z.p),
+                                                sc.z.ld, W.p, dw, W.ld, stream);
+        });
+        return Py_BuildValue("(iN)", int(st), THPVariable_Wrap(w));
+    });
+}
+
+// The arguments that the two block norms share, 0 .. 14:
+// R | None, Y | None, post, post_w, post_b, alpha, gate, pre, w, b, scale, shift, rows_per_sample | None, eps, H | None
+struct BlockNorm {
+    sq_block_norm norm{};
+    sq_dtype dt;
+    int64_t M, C;
+    Matrix Y, R, H;
+    at::Tensor h;
+    bool any_vector = false;
+
+    double number(const Args &a, int i)
+    {
+        const double v = PyFloat_AsDouble(a.a[i]);
+        if (v == -1.0 && PyErr_Occurred()) throw BadArgument();
+        return v;
+    }
+    // a vector over the channels, or one per sample (then [samples, C] or [C])
+    const void *vector(const Args &a, int i, const char *what, int64_t samples, int64_t *ld)
+    {
+        if (a.none(i)) return nullptr;
+        const at::Tensor &t = a.tensor(i);
+        const sq_dtype type = dtype_of(t);
+        if (any_vector && type != norm.p_dtype) refuse(PyExc_TypeError, "%s has another dtype than the vectors before it", what);
+        any_vector = true;
+        norm.p_dtype = type;
+        const int64_t d = t.dim();
+        if (d < 1 || d > 2 || (d == 2 && !ld) || t.size(d - 1) != C || (C > 1 && t.stride(d - 1) != 1)) refuse(PyExc_ValueError, "%s must be over the channels", what);
+        if (d == 2 && t.size(0) != 1 && t.size(0) < samples) refuse(PyExc_ValueError, "%s has fewer rows than there are samples", what);
+        if (ld) *ld = d == 2 && t.size(0) > 1 ? t.stride(0) : 0;
+        return on_device(t, what).data_ptr();
+    }
+    explicit BlockNorm(const Args &a)
+    {
+        if (a.none(0) && a.none(1)) refuse(PyExc_ValueError, "%s", "R and Y are both missing");
+        const at::Tensor &x = a.none(0) ? a.matrix(1) : a.matrix(0);
+        dt = dtype_of(x);
+        M = x.size(0), C = x.size(1);
+        if (!a.none(0)) R = Matrix(x, "R");
+        if (!a.none(1)) {
+            want_type(a.tensor(1), x.scalar_type(), "Y");
+            Y = Matrix(a.tensor(1), "Y", M, C);
+        }
+        int64_t T = M;
+        if (!a.none(12)) T = a.integer(12);
+        if (T < 1 && M > 0) refuse(PyExc_ValueError, "%s must be positive", "rows_per_sample");
+        const int64_t samples = M > 0 ? (M + T - 1) / T : 0;
+        norm.rows_per_sample = T;
+        norm.post = sq_norm(a.integer(2));
+        norm.post_w = vector(a, 3, "post_w", 1, nullptr);
+        norm.post_b = vector(a, 4, "post_b", 1, nullptr);
+        norm.alpha = float(number(a, 5));
+        norm.gate = vector(a, 6, "gate", samples, &norm.ld_gate);
+        norm.pre = sq_norm(a.integer(7));
+        norm.w = vector(a, 8, "w", 1, nullptr);
+        norm.b = vector(a, 9, "b", 1, nullptr);
+        norm.scale = vector(a, 10, "scale", samples, &norm.ld_scale);
+        norm.shift = vector(a, 11, "shift", samples, &norm.ld_shift);
+        norm.eps = float(number(a, 13));
+        if (!a.none(14)) {                               // H given: stored there
+            h = a.tensor(14);
+            want_type(h, x.scalar_type(), "H");
+            H = Matrix(h, "H", M, C);
+        } else if (!a.none(1)) {                         // a new one, where there is something to add
+            h = new_rows(M, C, x, x.scalar_type());
+            H = Matrix(h, "H");
+        } else {
+            h = x;                                       // h = r
+        }
+    }
+};
+
+// .., O | None, whether O is wanted -> (status, H, O | None)
+PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded("block_norm", n, 17, [&]() -> PyObject * {
+        const Args a{args};
+        const BlockNorm b(a);
+        const at::Tensor &x = a.none(0) ? a.matrix(1) : a.matrix(0);
+        at::Tensor o;
+        if (a.truth(16)) o = a.none(15) ? new_rows(b.M, b.C, x, x.scalar_type()) : a.tensor(15);
+        Matrix O;
+        if (o.defined()) {
+            want_type(o, x.scalar_type(), "out");
+            O = Matrix(o, "out", b.M, b.C);
+        }
+        void *stream = current_stream();
+        const sq_status st = without_gil([&] {
+            return segquant_block_norm(b.Y.p, b.Y.ld, b.R.p, b.R.ld, b.dt, b.M, b.C, &b.norm, b.H.p, b.H.ld, O.p, O.ld, stream);
+        });
+        return Py_BuildValue("(iNN)", int(st), THPVariable_Wrap(b.h), THPVariable_Wrap(o));
+    });
+}
+
+// .., seg, P, s_pos, s_neg | None, code, flags, c_pos | None, c_neg | None -> (status, H, c_pos, c_neg | None)
+PyObject *block_norm_quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded("block_norm_quantize", n, 23, [&]() -> PyObject * {
+        const Args a{args};
+        const BlockNorm b(a);
+        const at::Tensor &x = a.none(0) ? a.matrix(1) : a.matrix(0);
+        const sq_segtable *seg = a.seg(15);
+        const int64_t P = a.integer(16);
+        const float *sp = f32_vector(a, 17, P, "s_pos"), *sn = f32_vector(a, 18, P, "s_neg");
+        const sq_code code = sq_code(a.integer(19));
+        const uint32_t flags = uint32_t(a.integer(20));
+        const at::Tensor cp = a.none(21) ? new_codes(b.M, b.C, x) : a.tensor(21);
+        at::Tensor cn;
+        if (sn) cn = a.none(22) ? new_codes(b.M, b.C, x) : a.tensor(22);
+        want_type(cp, at::kByte, "c_pos");
+        const Matrix P1(cp, "c_pos", b.M, b.C);
+        Matrix P2;
+        if (cn.defined()) {
+            want_type(cn, at::kByte, "c_neg");
+            P2 = Matrix(cn, "c_neg", b.M, b.C);
+            if (P2.ld != P1.ld) refuse(PyExc_ValueError, "%s must have the pitch of c_pos", "c_neg");
+        }
+        void *stream = current_stream();
+        const sq_status st = without_gil([&] {
+            return segquant_block_norm_quantize(b.Y.p, b.Y.ld, b.R.p, b.R.ld, b.dt, b.M, b.C, &b.norm, b.H.p, b.H.ld, seg, sp, sn, code, flags, P1.p,
+                                                P2.p, P1.ld, stream);
+        });
+        return Py_BuildValue("(iNNN)", int(st), THPVariable_Wrap(b.h), THPVariable_Wrap(cp), THPVariable_Wrap(cn));
+    });
+}
+
 // address of a plan
 PyObject *plan_run(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -304,7 +575,9 @@ PyObject *plan_run(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define SQ_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SQ_METHOD(layer_forward), SQ_METHOD(quantize_act), SQ_METHOD(quantize_act_fused), SQ_METHOD(gemm),
-                         SQ_METHOD(quantize_per_row), SQ_METHOD(calib_scales), SQ_METHOD(quantize_weight), SQ_METHOD(unpack_w4), SQ_METHOD(plan_run), {nullptr, nullptr, 0, nullptr}};
+                         SQ_METHOD(quantize_per_row), SQ_METHOD(calib_scales), SQ_METHOD(quantize_weight), SQ_METHOD(unpack_w4), SQ_METHOD(plan_run),
+                         SQ_METHOD(w4_matvec), SQ_METHOD(quantize_w4_group), SQ_METHOD(dequantize_w4_group), SQ_METHOD(block_norm),
+                         SQ_METHOD(block_norm_quantize), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

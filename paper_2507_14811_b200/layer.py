@@ -78,8 +78,51 @@ class SegQuantLinear:
         Y, dump = out if dump_acc else (out, None)
         return Y, c_pos, c_neg, dump
 
+    def forward_block(self, R, X=None, Y: torch.Tensor | None = None, y_dtype=torch.bfloat16, **norm):
+        """The layer behind a block norm: (H, Y) with H = R + alpha gate post(X) the new residual stream and Y the layer of
+        norm(H) (1 + scale) + shift, whose values go to the GEMM as codes and never to device memory.  X: the output of the block
+        before (None at the start); norm: gate, alpha, post, norm, scale, shift, rows_per_sample .. of
+        binding.segquant_block_norm.  Calibrate the layer with such norms' outputs."""
+        M = (X if R is None else R).shape[0]
+        ldc = (self.K + 127) // 128 * 128
+        scratch = self.scratch_for(M)
+        codes = lambda at: scratch[at:at + M * ldc].view(M, ldc)[:, :self.K]
+        H, c_pos, c_neg = B.segquant_block_norm_quantize(
+            R, self.seg, self.s_pos, self.s_neg, self.code, Y=X, flags=self.flags, c_pos=codes(0),
+            c_neg=codes((M * ldc + 255) // 256 * 256) if self.dual else None, **norm)
+        if self.dual:
+            return H, B.segquant_dualscale_gemm(c_pos, c_neg, self.Wq, self.seg, self.code, self.s_pos, self.s_neg, self.s_w, self.bias,
+                                                self.workspace, y_dtype=y_dtype, Y=Y)
+        return H, B.segquant_seglinear_gemm(c_pos, self.Wq, self.seg, self.code, self.s_pos, self.s_w, self.bias, self.workspace,
+                                            y_dtype=y_dtype, Y=Y)
+
     def check_status(self):
         B.check_device_status(self.workspace)
+
+
+class W4GroupLinear:
+    """Linear layer for few rows with 4-bit weights, one scale (and zero-point) per output channel and group of inputs; the
+    activations stay real numbers.  The modulation projection of a block (one conditioning vector per sample), single tokens."""
+
+    def __init__(self, W: torch.Tensor, bias=None, group: int = 128, zero_points: bool = False, s_dtype=torch.float32, device="cuda"):
+        self.device = torch.device(device)
+        self.N, self.K = W.shape
+        self.group = group
+        Wd = W.to(self.device)
+        unit = 16 // Wd.element_size()
+        if Wd.stride(1) != 1 or Wd.stride(0) % unit or Wd.data_ptr() % 16:       # rows on 16-byte boundaries for the quantizer
+            buf = torch.empty((self.N, (self.K + unit - 1) // unit * unit), dtype=Wd.dtype, device=self.device)[:, :self.K]
+            Wd = buf.copy_(Wd)
+        self.Wq4, self.s_w, self.z_w = B.segquant_quantize_w4_group(Wd, group, s_dtype, zero_points)
+        self.bias = None if bias is None else bias.to(self.device, torch.float32).contiguous()
+
+    def forward(self, X: torch.Tensor, act=None, Y: torch.Tensor | None = None, y_dtype=torch.bfloat16) -> torch.Tensor:
+        """act(X) [M, K] -> Y [M, N]."""
+        return B.segquant_w4_matvec(X, self.Wq4, self.s_w, self.group, self.z_w, self.bias, act=act, y_dtype=y_dtype, Y=Y)
+
+    def weights(self, dtype=torch.bfloat16) -> torch.Tensor:
+        """The weights [N, K] that the codes stand for (for a library product where there are many rows)."""
+        return B.segquant_dequantize_w4_group(self.Wq4, self.s_w, self.group, self.K, self.z_w, dtype=dtype)
 
 
 def shard_rows(M: int, rank: int, world: int) -> tuple[int, int]:
