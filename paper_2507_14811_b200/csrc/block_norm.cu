@@ -6,10 +6,15 @@
 //   o = o (1 + scale[b]) + shift[b]     -> values, or the 8-bit codes of segquant_quantize_act
 //
 // Bound by memory: y and r are read once, h and o (or its codes) written once.  A row stays in registers from the load to the
-// store, spread over WPR warps with CH chunks of eight elements a lane: one warp per row needs shuffles alone for its sums, and is
-// taken where there are rows enough to fill the GPU; few rows are spread over more warps, which shortens each thread's chain.  Sums
-// are fp32; a layer norm's variance is that of the centred values, a second sweep over registers, so that a large mean costs no
-// digits.  The vectors of a sample come through L1, which they share with nothing: rows are loaded and stored around it.
+// store, spread over WPR warps with CH chunks of eight elements a lane, and a row group's next row is on its way while the current
+// one is worked on.  One warp per row needs shuffles alone for its sums and is taken where there are rows enough to fill the GPU; few rows are
+// spread over a block each, which shortens every thread's chain.  Sums are fp32; a layer norm's variance is that of the centred
+// values, a second sweep over registers, so that a large mean costs no digits.
+//
+// What is done per channel on either side is one multiply-add: h = r + (yn P + Q), o = hn A + B with P = alpha post_w gate,
+// Q = alpha post_b gate, A = w (1 + scale), B = b (1 + scale) + shift.  A block makes these vectors in shared memory for the sample that its rows
+// belong to; reading up to seven vectors of two types, aligned or not, for every row instead made a kernel of some 50 KB of
+// instructions, which waited for its own code (8858 x 1536 bf16, two RMS norms: 63.6 us; gated and modulated to codes 135 us).
 #include <cuda_bf16.h>
 #include <algorithm>
 #include <atomic>
@@ -21,17 +26,23 @@ namespace sq {
 
 enum : int { kOutValues = 0, kOutInt8 = 1, kOutInt8Dual = 2, kOutE4m3 = 3, kOutE4m3Dual = 4 };
 
+constexpr int kMaxVectorBytes = 220 * 1024;       // of the vectors in shared memory
+
 struct BlockNormParams {
     const void *Y, *R;
-    int64_t ldy, ldr, M;
-    int C;
+    int64_t ldy, ldr;
+    int M, C;
+    int ragged;                       // C is no multiple of 8
     int post, pre;
     const void *post_w, *post_b, *w, *b;
     const void *gate, *scale, *shift;
     int64_t ld_gate, ld_scale, ld_shift;
-    int64_t rows_per_sample;
+    int rows_per_sample;              // at most M
     int p_f32;                        // type of those vectors
     int vec;                          // bit i: vector i of post_w, post_b, w, b, gate, scale, shift may be read 16 bytes at a time
+    int has;                          // bits: which of P, Q, A, B there are
+    int sm_at[4];                     // where they lie in shared memory
+    int two_steps;                    // shared memory holds P and Q or A and B
     float alpha, eps, inv_c;
     void *H, *O;
     int64_t ldh, ldo;
@@ -48,6 +59,7 @@ namespace {
 template <typename T> struct Chunk;                     // eight elements as loaded
 template <> struct Chunk<float> { uint4 v[2]; };
 template <> struct Chunk<__nv_bfloat16> { uint4 v[1]; };
+struct Eight { float v[8]; };
 
 __device__ __forceinline__ uint4 load_stream(const void *p)            // read once: not kept in L1
 {
@@ -55,33 +67,16 @@ __device__ __forceinline__ uint4 load_stream(const void *p)            // read o
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+// Words of 16 bytes that hold at least one element of the row (rows start on 16-byte boundaries, so what else is in such a word
+// belongs to the same allocation); the others are zero.
 template <typename T>
 __device__ __forceinline__ void load_chunk(const T *row, int col, int C, Chunk<T> &c)
 {
-    constexpr int W = int(sizeof(T)) / 2;
-    if (col + 8 <= C) {
+    constexpr int W = int(sizeof(T)) / 2, PER = 16 / int(sizeof(T));
 #pragma unroll
-        for (int i = 0; i < W; i++) c.v[i] = load_stream(reinterpret_cast<const uint4 *>(row + col) + i);
-    } else {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            x[i] = 0.0f;
-            if (col + i < C) {
-                if (sizeof(T) == 4) x[i] = reinterpret_cast<const float *>(row)[col + i];
-                else x[i] = __uint_as_float(uint32_t(reinterpret_cast<const uint16_t *>(row)[col + i]) << 16);
-            }
-        }
-        if (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < W; i++)
-                c.v[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xFFFF0000u);
-            c.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+    for (int i = 0; i < W; i++) {
+        c.v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (col + i * PER < C) c.v[i] = load_stream(row + col + i * PER);
     }
 }
 template <typename T>
@@ -92,53 +87,120 @@ __device__ __forceinline__ void expand(const Chunk<T> &c, float (&x)[8])
     for (int i = 0; i < 8; i++)
         x[i] = sizeof(T) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
-// eight elements of a vector over the channels, `at` elements behind its start
-template <typename Tp>
-__device__ __forceinline__ void load_vector_of(const Tp *v, int left, bool wide, float (&x)[8])
+// elements behind the row's end become zero, for the sums
+__device__ __forceinline__ void cut(float (&x)[8], int left)
 {
-    if (wide && left >= 8) {
-        constexpr int W = int(sizeof(Tp)) / 2;
-        Chunk<Tp> c;
 #pragma unroll
-        for (int i = 0; i < W; i++) c.v[i] = __ldg(reinterpret_cast<const uint4 *>(v) + i);
-        expand(c, x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = i < left ? load1(v + i) : 0.0f;
-    }
+    for (int i = 0; i < 8; i++) x[i] = i < left ? x[i] : 0.0f;
 }
-__device__ __forceinline__ void load_vector(const BlockNormParams &prm, const void *v, int64_t at, int col, int which, float (&x)[8])
+template <typename T>
+__device__ __noinline__ void store_tail(T *p, int left, Eight x)
 {
-    const bool wide = (prm.vec >> which) & 1;
-    if (prm.p_f32) load_vector_of(static_cast<const float *>(v) + at + col, prm.C - col, wide, x);
-    else load_vector_of(static_cast<const __nv_bfloat16 *>(v) + at + col, prm.C - col, wide, x);
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < left) {
+            if (sizeof(T) == 4) reinterpret_cast<float *>(p)[i] = x.v[i];
+            else reinterpret_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(x.v[i]);
+        }
 }
 template <typename T>
 __device__ __forceinline__ void store_chunk(T *row, int col, int C, const float (&x)[8])
 {
     if (col + 8 <= C) {
-        uint32_t w[2 * sizeof(T)];
         if (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) w[i % (2 * sizeof(T))] = __float_as_uint(x[i]);
+            reinterpret_cast<float4 *>(row + col)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4 *>(row + col)[1] = make_float4(x[4], x[5], x[6], x[7]);
         } else {
+            uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
                 w[i] = *reinterpret_cast<const uint32_t *>(&b);
             }
+            *reinterpret_cast<uint4 *>(row + col) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+    } else {
+        Eight e;
 #pragma unroll
-        for (int i = 0; i < int(sizeof(T)) / 2; i++)
-            reinterpret_cast<uint4 *>(row + col)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        for (int i = 0; i < 8; i++) e.v[i] = x[i];
+        store_tail(row + col, C - col, e);
+    }
+}
+
+// ---- the vectors of a sample
+enum : int { kP = 0, kQ = 1, kA = 2, kB = 3 };
+__device__ __forceinline__ float vector1(const BlockNormParams &prm, const void *v, int64_t at)
+{
+    return prm.p_f32 ? __ldg(static_cast<const float *>(v) + at) : load1(static_cast<const __nv_bfloat16 *>(v) + at);
+}
+// eight channels of one of the seven vectors; `absent` where it is not there
+__device__ __forceinline__ void vector8(const BlockNormParams &prm, const void *v, int64_t at, int which, int left, float absent, float (&x)[8])
+{
+    if (!v) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = absent;
+    } else if (((prm.vec >> which) & 1) && left >= 8) {
+        if (prm.p_f32) {
+            Chunk<float> c;
+#pragma unroll
+            for (int i = 0; i < 2; i++) c.v[i] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(v) + at) + i);
+            expand(c, x);
+        } else {
+            Chunk<__nv_bfloat16> c;
+            c.v[0] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(v) + at));
+            expand(c, x);
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (col + i < C) {
-                if (sizeof(T) == 4) reinterpret_cast<float *>(row)[col + i] = x[i];
-                else reinterpret_cast<__nv_bfloat16 *>(row)[col + i] = __float2bfloat16_rn(x[i]);
-            }
+        for (int i = 0; i < 8; i++) x[i] = i < left ? vector1(prm, v, at + i) : 0.0f;
     }
+}
+__device__ __forceinline__ void put8(float *p, const float (&x)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void get8(const float *p, float (&x)[8])
+{
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+// P and Q
+__device__ __forceinline__ void make_post(const BlockNormParams &prm, float *sm, int64_t sample, int col)
+{
+    if (!(prm.has & (1 << kP | 1 << kQ))) return;
+    const int left = prm.C - col;
+    float w[8], b[8], g[8];
+    vector8(prm, prm.post_w, col, 0, left, 1.0f, w);
+    vector8(prm, prm.post_b, col, 1, left, 0.0f, b);
+    vector8(prm, prm.gate, sample * prm.ld_gate + col, 4, left, 1.0f, g);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        g[i] *= prm.alpha;
+        w[i] *= g[i];
+        b[i] *= g[i];
+    }
+    if (prm.has >> kP & 1) put8(sm + prm.sm_at[kP] + col, w);
+    if (prm.has >> kQ & 1) put8(sm + prm.sm_at[kQ] + col, b);
+}
+// A and B
+__device__ __forceinline__ void make_pre(const BlockNormParams &prm, float *sm, int64_t sample, int col)
+{
+    if (!(prm.has & (1 << kA | 1 << kB))) return;
+    const int left = prm.C - col;
+    float w[8], b[8], s[8], t[8];
+    vector8(prm, prm.w, col, 2, left, 1.0f, w);
+    vector8(prm, prm.b, col, 3, left, 0.0f, b);
+    vector8(prm, prm.scale, sample * prm.ld_scale + col, 5, left, 0.0f, s);
+    vector8(prm, prm.shift, sample * prm.ld_shift + col, 6, left, 0.0f, t);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float f = 1.0f + s[i];
+        w[i] *= f;
+        b[i] = fmaf(b[i], f, t[i]);
+    }
+    if (prm.has >> kA & 1) put8(sm + prm.sm_at[kA] + col, w);
+    if (prm.has >> kB & 1) put8(sm + prm.sm_at[kB] + col, b);
 }
 
 // Sum over the WPR warps of a row, the same bits in every lane.  `red`: WPR floats of the row, another buffer each time.
@@ -158,7 +220,7 @@ __device__ __forceinline__ float row_sum(float v, float *red, int warp_of_row, i
 
 // x <- normalised x (elements behind the row's end are zero before, and do not count)
 template <int CH, int WPR>
-__device__ __forceinline__ void normalise(float (&x)[CH][8], int kind, int C, float inv_c, float eps, const int (&col)[CH], float *red,
+__device__ __forceinline__ void normalise(float (&x)[CH][8], int kind, const BlockNormParams &prm, const int (&col)[CH], float *red,
                                           int warp_of_row, int row_of_block)
 {
     if (kind == SQ_NORM_LAYER) {
@@ -167,11 +229,14 @@ __device__ __forceinline__ void normalise(float (&x)[CH][8], int kind, int C, fl
         for (int c = 0; c < CH; c++)
 #pragma unroll
             for (int i = 0; i < 8; i++) s += x[c][i];
-        const float mean = row_sum<WPR>(s, red, warp_of_row, row_of_block) * inv_c;
+        const float mean = row_sum<WPR>(s, red, warp_of_row, row_of_block) * prm.inv_c;
 #pragma unroll
-        for (int c = 0; c < CH; c++)
+        for (int c = 0; c < CH; c++) {
+            const float m = col[c] < prm.C ? mean : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[c][i] = col[c] + i < C ? x[c][i] - mean : 0.0f;
+            for (int i = 0; i < 8; i++) x[c][i] -= m;
+            if (prm.ragged) cut(x[c], prm.C - col[c]);
+        }
         red += WPR;
     }
     float q = 0.0f;
@@ -179,197 +244,252 @@ __device__ __forceinline__ void normalise(float (&x)[CH][8], int kind, int C, fl
     for (int c = 0; c < CH; c++)
 #pragma unroll
         for (int i = 0; i < 8; i++) q = fmaf(x[c][i], x[c][i], q);
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR>(q, red, warp_of_row, row_of_block), inv_c, eps));
+    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR>(q, red, warp_of_row, row_of_block), prm.inv_c, prm.eps));
 #pragma unroll
     for (int c = 0; c < CH; c++)
 #pragma unroll
         for (int i = 0; i < 8; i++) x[c][i] *= rstd;
 }
 
-template <typename T, int OUT, int CH, int WPR, int RPB>
-__global__ void __launch_bounds__(WPR * RPB * 32) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
+// Codes of a chunk that crosses a segment bound or the row's end, or whose scale is outside the fast form: element by element.
+template <int CODE, int MODE>
+__device__ __noinline__ void codes_tail(const BlockNormParams &prm, int col, Eight o, uint8_t *dp, uint8_t *dn)
 {
-    constexpr bool CODES = OUT != kOutValues, DUAL = OUT == kOutInt8Dual || OUT == kOutE4m3Dual;
+    int q = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if (col + i >= prm.C) return;
+        while (q + 1 < prm.sb.P && col + i >= prm.sb.kb[q + 1]) q++;
+        uint32_t bp, bn;
+        quant1<CODE, MODE>(o.v[i], __ldg(prm.s_pos + q), MODE == kDual ? __ldg(prm.s_neg + q) : 1.0f, 0, prm.lo, prm.hi, bp, bn);
+        dp[i] = uint8_t(bp);
+        if (MODE == kDual) dn[i] = uint8_t(bn);
+    }
+}
+
+// Threads of a block: RPB rows at a time, WPR warps each.  RPB > 1: the block's rows share the vectors of their sample in shared memory;
+// RPB == 1: every thread makes and reads those of its own channels, so nothing has to wait.
+template <typename T, int OUT, int CH, int WPR, int RPB>
+__global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
+{
+    constexpr bool CODES = OUT != kOutValues, DUAL = OUT == kOutInt8Dual || OUT == kOutE4m3Dual, SHARED = RPB > 1;
     constexpr int CODE = OUT >= kOutE4m3 ? SQ_CODE_E4M3 : SQ_CODE_INT8, MODE = DUAL ? kDual : kSingle;
+    extern __shared__ __align__(16) float sm[];
     __shared__ SegConst sm_pos[CODES ? SQ_MAX_P : 1], sm_neg[CODES && DUAL ? SQ_MAX_P : 1];
     __shared__ float sm_red[WPR > 1 ? RPB * 4 * WPR : 1];       // four sums a row: mean and variance, twice
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row_of_block = warp / WPR, warp_of_row = warp % WPR;
     const int C = prm.C;
+    const T *Y = static_cast<const T *>(prm.Y), *R = static_cast<const T *>(prm.R);
+    // this block's rows, and its row group's first
+    const int r0 = int(int64_t(blockIdx.x) * prm.M / gridDim.x), r1 = int((int64_t(blockIdx.x) + 1) * prm.M / gridDim.x);
+    int m = r0 + row_of_block;
     int col[CH];
+    Chunk<T> y[CH], r[CH];
+    auto fetch = [&](int row) {
+#pragma unroll
+        for (int c = 0; c < CH; c++) {
+            if (Y) load_chunk(Y + row * prm.ldy, col[c], C, y[c]);
+            if (R) load_chunk(R + row * prm.ldr, col[c], C, r[c]);
+        }
+    };
 #pragma unroll
     for (int c = 0; c < CH; c++) col[c] = ((c * WPR + warp_of_row) * 32 + lane) * 8;
-    uint32_t seg[CODES ? CH : 1];                              // K-segment of a chunk's first element; bit 31: the chunk crosses a bound
+    if (m < r1) fetch(m);
+
+    uint32_t seg[CODES ? CH : 1];                              // K-segment of a chunk; bit 31: it is done element by element
     if (CODES) {
         for (int p = threadIdx.x; p < prm.sb.P; p += blockDim.x) {
             sm_pos[p] = seg_const(__ldg(prm.s_pos + p));
             if (DUAL) sm_neg[p] = seg_const(__ldg(prm.s_neg + p));
         }
+        __syncthreads();
 #pragma unroll
         for (int c = 0; c < CH; c++) {
             int p = 0;
             while (p + 1 < prm.sb.P && col[c] >= prm.sb.kb[p + 1]) p++;
-            seg[c] = uint32_t(p) | (min(col[c] + 8, C) > prm.sb.kb[p + 1] ? 0x80000000u : 0u);
+            const bool fast = col[c] + 8 <= prm.sb.kb[p + 1] && sm_pos[p].fast && (!DUAL || sm_neg[p].fast) &&
+                              !(CODE == SQ_CODE_INT8 && DUAL && prm.lo != -128);
+            seg[c] = uint32_t(p) | (fast ? 0u : 0x80000000u);
         }
-        __syncthreads();
     }
     float *red = sm_red + (WPR > 1 ? row_of_block * 4 * WPR : 0);
-    const T *Y = static_cast<const T *>(prm.Y), *R = static_cast<const T *>(prm.R);
-    for (int64_t m = int64_t(blockIdx.x) * RPB + row_of_block; m < prm.M; m += int64_t(gridDim.x) * RPB) {
-        Chunk<T> y[CH], r[CH];
-#pragma unroll
-        for (int c = 0; c < CH; c++) {
-            if (Y && col[c] < C) load_chunk(Y + m * prm.ldy, col[c], C, y[c]);
-            if (R && col[c] < C) load_chunk(R + m * prm.ldr, col[c], C, r[c]);
-        }
-        const int64_t sample = m / prm.rows_per_sample;
-        float h[CH][8];
-        if (Y) {
-#pragma unroll
-            for (int c = 0; c < CH; c++) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) h[c][i] = 0.0f;
-                if (col[c] < C) expand(y[c], h[c]);
+    int start = r0;
+    for (int sample = r0 / prm.rows_per_sample; start < r1; sample++) {
+        const int end = int(min(int64_t(r1), (int64_t(sample) + 1) * prm.rows_per_sample));
+        if (SHARED) {
+            if (start != r0) __syncthreads();                  // the last sample's vectors have been used
+            for (int k = int(threadIdx.x) * 8; k < C; k += int(blockDim.x) * 8) {
+                make_post(prm, sm, sample, k);
+                make_pre(prm, sm, sample, k);
             }
-            if (prm.post != SQ_NORM_NONE)
-                normalise<CH, WPR>(h, prm.post, C, prm.inv_c, prm.eps, col, red, warp_of_row, row_of_block);
-#pragma unroll
+            __syncthreads();
+        } else if (!prm.two_steps) {
+#pragma unroll 1
             for (int c = 0; c < CH; c++) {
-                if (col[c] >= C) continue;
-                float v[8];
-                if (prm.post_w) {
-                    load_vector(prm, prm.post_w, 0, col[c], 0, v);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) h[c][i] *= v[i];
-                }
-                if (prm.post_b) {
-                    load_vector(prm, prm.post_b, 0, col[c], 1, v);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) h[c][i] += v[i];
-                }
-                if (prm.gate) {
-                    load_vector(prm, prm.gate, sample * prm.ld_gate, col[c], 4, v);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) h[c][i] *= v[i];
-                }
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) x[i] = 0.0f;
-                if (R) expand(r[c], x);
-#pragma unroll
-                for (int i = 0; i < 8; i++) h[c][i] = fmaf(prm.alpha, h[c][i], x[i]);
-                if (prm.H) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < CH; c++) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) h[c][i] = 0.0f;
-                if (col[c] < C) {
-                    expand(r[c], h[c]);
-                    if (prm.H) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
-                }
+                const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
+                if (k < C) make_post(prm, sm, sample, k), make_pre(prm, sm, sample, k);
             }
         }
-        if (CODES || prm.O) {
-        // behind the row's end everything is zero, for the sums
+        for (; m < end; m += RPB) {
+            float h[CH][8];
+            if (Y) {
 #pragma unroll
-        for (int c = 0; c < CH; c++)
+                for (int c = 0; c < CH; c++) expand(y[c], h[c]);
+                if (prm.post != SQ_NORM_NONE) {
+                    if (prm.ragged) {
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (col[c] + i >= C) h[c][i] = 0.0f;
-        if (prm.pre != SQ_NORM_NONE)
-            normalise<CH, WPR>(h, prm.pre, C, prm.inv_c, prm.eps, col, red + 2 * WPR * (WPR > 1), warp_of_row, row_of_block);
+                        for (int c = 0; c < CH; c++) cut(h[c], C - col[c]);
+                    }
+                    normalise<CH, WPR>(h, prm.post, prm, col, red, warp_of_row, row_of_block);
+                }
+                if (!SHARED && prm.two_steps) {
+#pragma unroll 1
+                    for (int c = 0; c < CH; c++) {
+                        const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
+                        if (k < C) make_post(prm, sm, sample, k);
+                    }
+                }
 #pragma unroll
-        for (int c = 0; c < CH; c++) {
-            if (col[c] >= C) continue;
-            float v[8], o[8];
+                for (int c = 0; c < CH; c++) {
+                    if (col[c] >= C) continue;
+                    float v[8], x[8];
+                    if (R) {
+                        expand(r[c], x);
+                    } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = h[c][i];
-            if (prm.w) {
-                load_vector(prm, prm.w, 0, col[c], 2, v);
+                        for (int i = 0; i < 8; i++) x[i] = 0.0f;
+                    }
+                    if (prm.has >> kQ & 1) {
+                        get8(sm + prm.sm_at[kQ] + col[c], v);
 #pragma unroll
-                for (int i = 0; i < 8; i++) o[i] *= v[i];
-            }
-            if (prm.b) {
-                load_vector(prm, prm.b, 0, col[c], 3, v);
+                        for (int i = 0; i < 8; i++) x[i] += v[i];
+                    }
+                    if (prm.has >> kP & 1) {
+                        get8(sm + prm.sm_at[kP] + col[c], v);
 #pragma unroll
-                for (int i = 0; i < 8; i++) o[i] += v[i];
-            }
-            if (prm.scale) {
-                load_vector(prm, prm.scale, sample * prm.ld_scale, col[c], 5, v);
+                        for (int i = 0; i < 8; i++) h[c][i] = fmaf(h[c][i], v[i], x[i]);
+                    } else {
 #pragma unroll
-                for (int i = 0; i < 8; i++) o[i] *= 1.0f + v[i];
-            }
-            if (prm.shift) {
-                load_vector(prm, prm.shift, sample * prm.ld_shift, col[c], 6, v);
-#pragma unroll
-                for (int i = 0; i < 8; i++) o[i] += v[i];
-            }
-            if (!CODES) {
-                store_chunk(static_cast<T *>(prm.O) + m * prm.ldo, col[c], C, o);
+                        for (int i = 0; i < 8; i++) h[c][i] += x[i];
+                    }
+                }
             } else {
-                const int p = int(seg[c] & 0x7FFFFFFFu);
-                const SegConst cp = sm_pos[p], cn = DUAL ? sm_neg[p] : cp;
-                uint32_t wp[2], wn[2] = {0, 0};
-                const bool fast = !(seg[c] >> 31) && cp.fast && (!DUAL || cn.fast) && !(CODE == SQ_CODE_INT8 && DUAL && prm.lo != -128);
-                if (fast) {
-                    const float a[4] = {o[0], o[1], o[2], o[3]}, b[4] = {o[4], o[5], o[6], o[7]};
-                    quant4<CODE, MODE>(a, cp, cn, float(prm.hi), 0, wp[0], wn[0]);
-                    quant4<CODE, MODE>(b, cp, cn, float(prm.hi), 0, wp[1], wn[1]);
-                } else {
-                    wp[0] = wp[1] = 0;
-                    int q = p;
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        if (col[c] + i >= C) break;
-                        while (q + 1 < prm.sb.P && col[c] + i >= prm.sb.kb[q + 1]) q++;
-                        uint32_t bp, bn;
-                        quant1<CODE, MODE>(o[i], sm_pos[q].s, DUAL ? sm_neg[q].s : 1.0f, 0, prm.lo, prm.hi, bp, bn);
-                        wp[i / 4] |= bp << (8 * (i & 3));
-                        wn[i / 4] |= bn << (8 * (i & 3));
+                for (int c = 0; c < CH; c++) expand(r[c], h[c]);
+            }
+            // the next row's loads go out before anything is stored; it is never a row that this group still has to write
+            if (m + RPB < r1) fetch(m + RPB);
+            if (prm.H) {
+#pragma unroll
+                for (int c = 0; c < CH; c++)
+                    if (col[c] < C) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
+            }
+            if (CODES || prm.O) {
+                if (prm.ragged) {
+#pragma unroll
+                    for (int c = 0; c < CH; c++) cut(h[c], C - col[c]);
+                }
+                if (prm.pre != SQ_NORM_NONE)
+                    normalise<CH, WPR>(h, prm.pre, prm, col, red + 2 * WPR * (WPR > 1), warp_of_row, row_of_block);
+                if (!SHARED && prm.two_steps) {
+#pragma unroll 1
+                    for (int c = 0; c < CH; c++) {
+                        const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
+                        if (k < C) make_pre(prm, sm, sample, k);
                     }
                 }
-                uint8_t *dp = prm.c_pos + m * prm.ldc + col[c], *dn = DUAL ? prm.c_neg + m * prm.ldc + col[c] : nullptr;
-                if (col[c] + 8 <= C) {
-                    *reinterpret_cast<uint2 *>(dp) = make_uint2(wp[0], wp[1]);
-                    if (DUAL) *reinterpret_cast<uint2 *>(dn) = make_uint2(wn[0], wn[1]);
-                } else {
-                    for (int i = 0; col[c] + i < C; i++) {
-                        dp[i] = uint8_t(wp[i / 4] >> (8 * (i & 3)));
-                        if (DUAL) dn[i] = uint8_t(wn[i / 4] >> (8 * (i & 3)));
+#pragma unroll
+                for (int c = 0; c < CH; c++) {
+                    if (col[c] >= C) continue;
+                    float v[8];
+                    if (prm.has >> kA & 1) {
+                        get8(sm + prm.sm_at[kA] + col[c], v);
+#pragma unroll
+                        for (int i = 0; i < 8; i++) h[c][i] *= v[i];
+                    }
+                    if (prm.has >> kB & 1) {
+                        get8(sm + prm.sm_at[kB] + col[c], v);
+#pragma unroll
+                        for (int i = 0; i < 8; i++) h[c][i] += v[i];
+                    }
+                    if (!CODES) {
+                        store_chunk(static_cast<T *>(prm.O) + m * prm.ldo, col[c], C, h[c]);
+                    } else {
+                        uint8_t *dp = prm.c_pos + m * prm.ldc + col[c], *dn = DUAL ? prm.c_neg + m * prm.ldc + col[c] : nullptr;
+                        if (seg[c] >> 31) {
+                            Eight e;
+#pragma unroll
+                            for (int i = 0; i < 8; i++) e.v[i] = h[c][i];
+                            codes_tail<CODE, MODE>(prm, col[c], e, dp, dn);
+                        } else {
+                            const SegConst cp = sm_pos[seg[c]], cn = DUAL ? sm_neg[seg[c]] : cp;
+                            const float a[4] = {h[c][0], h[c][1], h[c][2], h[c][3]}, b[4] = {h[c][4], h[c][5], h[c][6], h[c][7]};
+                            uint32_t wp[2], wn[2];
+                            quant4<CODE, MODE>(a, cp, cn, float(prm.hi), 0, wp[0], wn[0]);
+                            quant4<CODE, MODE>(b, cp, cn, float(prm.hi), 0, wp[1], wn[1]);
+                            *reinterpret_cast<uint2 *>(dp) = make_uint2(wp[0], wp[1]);
+                            if (DUAL) *reinterpret_cast<uint2 *>(dn) = make_uint2(wn[0], wn[1]);
+                        }
                     }
                 }
             }
+            // the next row's first sums overwrite words that a slower warp may still be reading
+            if (WPR > 1) asm volatile("bar.sync %0, %1;" ::"r"(row_of_block + 1), "n"(WPR * 32) : "memory");
         }
-        }
-        // the next row's first sums overwrite words that a slower warp may still be reading
-        if (WPR > 1) asm volatile("bar.sync %0, %1;" ::"r"(row_of_block + 1), "n"(WPR * 32) : "memory");
+        start = end;
     }
 }
 
-// One shape: CH chunks a lane, WPR warps per row, RPB rows per block.
+// One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1536 bf16 (1024 fp32) channels
+// where there are rows enough for that, two and four up to four times as many, then a block per row; few rows get a block each, and
+// so do rows that each have vectors of their own.
 template <typename T, int OUT>
-sq_status run_shape(const BlockNormParams &p, cudaStream_t st)
+sq_status run_shape(BlockNormParams p, cudaStream_t st)
 {
     int dev = -1, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return SQ_ERR_CUDA;
-    auto go = [&](auto kernel, int rpb, int threads) {
-        int per_sm = 2048 / threads;
+    const int pitch = (p.C + 7) / 8 * 8;                 // floats of a vector in shared memory
+    auto go = [&](auto kernel, int wpr, int rpb) {
+        const int threads = wpr * rpb * 32;
+        int vectors = 0;
+        for (int i = 0; i < 4; i++)
+            if (p.has >> i & 1) p.sm_at[i] = pitch * vectors++;
+        if (rpb == 1 && vectors == 4 && 4 * pitch * 4 > kMaxVectorBytes) {      // then two at a time, made anew for every row
+            p.two_steps = 1;
+            p.sm_at[kA] = 0, p.sm_at[kB] = pitch;
+            vectors = 2;
+        }
+        const size_t smem = size_t(vectors) * pitch * 4;
+        if (smem > 48 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxVectorBytes);
+            if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
+        }
+        const int per_sm = rpb > 1 ? 2 : std::max(1, std::min(1024 / threads, int(kMaxVectorBytes / (smem + 1024))));
         const int64_t blocks = std::min<int64_t>((p.M + rpb - 1) / rpb, int64_t(sms) * per_sm);
-        kernel<<<unsigned(blocks), threads, 0, st>>>(p);
+        kernel<<<unsigned(blocks), threads, smem, st>>>(p);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
         count_launch();
         return SQ_OK;
     };
     const int chunks = (p.C + 7) / 8;
-#define SQ_SHAPE(CH, WPR, RPB) return go(block_norm_kernel<T, OUT, CH, WPR, RPB>, RPB, WPR * RPB * 32)
-    const bool many = p.M >= int64_t(sms) * 8;
-    if (many && chunks <= 32) SQ_SHAPE(1, 1, 8);
-    if (many && chunks <= 64) SQ_SHAPE(2, 1, 8);
-    if (many && chunks <= 128) SQ_SHAPE(4, 1, 8);
-    if (many && chunks <= 192) SQ_SHAPE(6, 1, 8);
+    constexpr bool HALF = sizeof(T) == 2;
+#define SQ_SHAPE(CH, WPR, RPB) return go(block_norm_kernel<T, OUT, CH, WPR, RPB>, WPR, RPB)
+    if (p.M >= int64_t(sms) * 8 && p.rows_per_sample >= 16) {
+        if (chunks <= 32) SQ_SHAPE(1, 1, 8);
+        if (chunks <= 64) SQ_SHAPE(2, 1, 8);
+        if (chunks <= 96) SQ_SHAPE(3, 1, 8);
+        if (chunks <= 128) SQ_SHAPE(4, 1, 8);
+        if constexpr (HALF) {
+            if (chunks <= 160) SQ_SHAPE(5, 1, 8);
+            if (chunks <= 192) SQ_SHAPE(6, 1, 8);
+        } else {
+            if (chunks <= 192) SQ_SHAPE(3, 2, 4);
+        }
+        if (chunks <= 256) SQ_SHAPE(4, 2, 4);
+        if (chunks <= 512) SQ_SHAPE(4, 4, 2);
+    }
     if (chunks <= 128) SQ_SHAPE(1, 4, 1);
     if (chunks <= 256) SQ_SHAPE(2, 4, 1);
     if (chunks <= 512) SQ_SHAPE(2, 8, 1);
@@ -397,12 +517,14 @@ sq_status launch_block_norm(const BlockNormArgs &a, cudaStream_t st)
     BlockNormParams p{};
     const sq_block_norm &n = *a.norm;
     const size_t ps = n.p_dtype == SQ_F32 ? 4 : 2;
-    p.Y = a.Y; p.R = a.R; p.ldy = a.ldy; p.ldr = a.ldr; p.M = a.M; p.C = int(a.C);
+    p.Y = a.Y; p.R = a.R; p.ldy = a.ldy; p.ldr = a.ldr; p.M = int(a.M); p.C = int(a.C); p.ragged = a.C % 8 != 0;
     p.post = n.post; p.pre = n.pre;
     p.post_w = n.post_w; p.post_b = n.post_b; p.w = n.w; p.b = n.b;
     p.gate = n.gate; p.scale = n.scale; p.shift = n.shift;
     p.ld_gate = n.ld_gate; p.ld_scale = n.ld_scale; p.ld_shift = n.ld_shift;
-    p.rows_per_sample = n.rows_per_sample;
+    p.rows_per_sample = int(std::min(n.rows_per_sample, a.M));
+    if (a.Y) p.has |= (n.post_w || n.gate || n.alpha != 1.0f) << 0 | (n.post_b != nullptr) << 1;
+    if (a.O || a.c_pos) p.has |= (n.w || n.scale) << 2 | (n.b || n.shift) << 3;
     p.vec = wide(n.post_w, 0, ps) | wide(n.post_b, 0, ps) << 1 | wide(n.w, 0, ps) << 2 | wide(n.b, 0, ps) << 3 |
             wide(n.gate, n.ld_gate, ps) << 4 | wide(n.scale, n.ld_scale, ps) << 5 | wide(n.shift, n.ld_shift, ps) << 6;
     p.alpha = n.alpha; p.eps = n.eps; p.inv_c = 1.0f / float(a.C);

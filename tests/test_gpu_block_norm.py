@@ -22,15 +22,20 @@ class Err:
     def __init__(self, v, e=None):
         self.v, self.e = v, torch.zeros_like(v) if e is None else e
 
-    def times(self, o):
-        o = o if isinstance(o, Err) else Err(o)
-        v = self.v * o.v
-        return Err(v, self.e * o.v.abs() + o.e * self.v.abs() + U * v.abs())
-
-    def plus(self, o):
-        o = o if isinstance(o, Err) else Err(o)
-        v = self.v + o.v
-        return Err(v, self.e + o.e + U * v.abs())
+    def linear(self, factors, terms):
+        """self times the factors plus the terms (each a list of factors), in any order that takes at most six roundings on the
+        way of each product or term to the result: 6 u of the sum of their magnitudes.  (Here: at most two products of the factors
+        among themselves, or one sum and one product, one with self, and two additions.)"""
+        scale = torch.ones_like(self.v)
+        for f in factors:
+            scale = scale * f
+        v, mags = self.v * scale, (self.v * scale).abs()
+        for t in terms:
+            x = torch.ones_like(self.v)
+            for f in t:
+                x = x * f
+            v, mags = v + x, mags + x.abs()
+        return Err(v, self.e * scale.abs() + 6 * U * mags)
 
     def normed(self, kind, eps):
         if kind == "none":
@@ -56,24 +61,17 @@ def spread(v, rows, T):
 def reference(R, Y, a):
     M, C = (Y if R is None else R).shape
     T = a.get("rows_per_sample") or M
+    get = lambda *names: [spread(a[k], M, T) for k in names if a.get(k) is not None]
     if Y is None:
         h = Err(R.double())
     else:
         u = Err(Y.double()).normed(a.get("post") or "none", a["eps"])
-        for k, f in (("post_w", "times"), ("post_b", "plus"), ("gate", "times")):
-            if a.get(k) is not None:
-                u = getattr(u, f)(spread(a[k], M, T))
-        alpha = float(torch.tensor(a.get("alpha", 1.0), dtype=F32))
-        h = u.times(torch.full_like(u.v, alpha)).plus(torch.zeros_like(u.v) if R is None else R.double())
-    o = h.normed(a.get("norm") or "none", a["eps"])
-    for k, f in (("w", "times"), ("b", "plus")):
-        if a.get(k) is not None:
-            o = getattr(o, f)(spread(a[k], M, T))
-    if a.get("scale") is not None:
-        o = o.times(Err(torch.ones_like(o.v)).plus(spread(a["scale"], M, T).expand_as(o.v)))
-    if a.get("shift") is not None:
-        o = o.plus(spread(a["shift"], M, T))
-    return h, o
+        alpha = [torch.tensor(a.get("alpha", 1.0), dtype=F32, device=DEV).double()]
+        terms = ([] if a.get("post_b") is None else [get("post_b", "gate") + alpha]) + ([] if R is None else [[R.double()]])
+        h = u.linear(get("post_w", "gate") + alpha, terms)
+    modulate = [1.0 + v for v in get("scale")]
+    terms = ([] if a.get("b") is None else [get("b") + modulate]) + ([] if a.get("shift") is None else [get("shift")])
+    return h, h.normed(a.get("norm") or "none", a["eps"]).linear(get("w") + modulate, terms)
 
 
 def check_values(got, want, what):
