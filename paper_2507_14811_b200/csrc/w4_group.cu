@@ -250,23 +250,24 @@ __global__ void __launch_bounds__(256) dequantize_w4_group_kernel(const __grid_c
 // ---------------------------------------------------------------------------------------------- matrix-vector product
 
 constexpr int kWarps = 16;
-constexpr int kTileN = 16;           // channels of a warp: the MMA's rows
+constexpr int kTileN = 16;           // channels of a tile: the MMA's rows
 constexpr int kUnitK = 256;          // codes per channel and ring stage: 128 bytes
 constexpr int kUnitBytes = kTileN * kUnitK / 2;
-constexpr int kMaxStages = 4;         // of a warp's ring; 2 or 3 where the activations leave no room for more
-constexpr int kRedPitch = 20;        // floats per column of a warp's partial sums (16 used; 20 keeps the stores off one bank)
+constexpr int kMaxStages = 4;        // of a warp's ring; 2 or 3 where the activations leave no room for more
+constexpr int kRedPitch = 20;        // floats per column of a tile's sums (16 used; 20 keeps the stores off one bank)
 constexpr int kMaxCols = 32;
 
 struct MatvecParams {
     const void *X;
     int64_t ldx;
     int M, rows;                     // rows of X, rows of one pass (grid.y)
-    int64_t K;
-    int x_f32, x_wide, act, parts;   // parts: bf16 terms per activation (1, or 3 for fp32 values)
+    int K;
+    int x_f32, x_wide, act, parts;   // parts: bf16 terms per activation
     const uint8_t *W4;
-    int64_t ldw, N, row_bytes;
-    int group;
-    int64_t groups;
+    int64_t ldw;
+    int N, row_bytes;
+    int units_group;                 // units of a long group (short ones: 1)
+    int groups;
     const uint8_t *s;
     int s_bytes;                     // 4 or 2
     int64_t lds;                     // bytes
@@ -276,13 +277,13 @@ struct MatvecParams {
     void *Y;
     int y_f32;
     int64_t ldy;
-    int units, cl, wk, wk_shift;     // K: units in all, CTAs of a cluster, warps of a CTA that share it
-    int units_cta, units_warp;
-    int64_t tiles;                   // of 16 * (16 / wk) channels
-    int clusters;
+    int cl;                          // CTAs of a cluster, which share K
+    int units, units_cta;            // of K, of a CTA
+    int tiles, clusters;
+    int tiles_round;                 // tiles whose sums fit in shared memory
     int cols;                        // columns in use: rows * parts
     int stages;
-    uint32_t stage_bytes, z_off, x_off, red_off, red_bytes;
+    uint32_t stage_bytes, z_off, x_off, red_off, head_off;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -313,33 +314,41 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t word, int i, uint32_t off
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(v), "r"(offset));
     return d;
 }
-__device__ __forceinline__ float act1(float x, int act)
+// Two activations as sums of bf16 terms: truncations of 8 significant bits each, three of which hold an fp32 value exactly (down to
+// 2^-133, where bf16 ends), or a truncation and a rounded rest, 2^-17 of the value off, which is taken where the output is bf16.  What is
+// infinite keeps to the first term; a NaN is one in all.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
+__device__ __forceinline__ float truncated_rest(float x)
 {
-    float a, b;
-    if (act == SQ_ACT_NONE) return x;
-    unpack2(act == SQ_ACT_SILU ? silu2(x, x) : gelu2(x, x), a, b);
-    return a;
+    const float r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    return fabsf(x) == __int_as_float(0x7F800000) ? 0.0f : r;
 }
-// an fp32 value as the sum of three bf16 numbers, exactly (truncations of 8 significant bits each); what is not finite keeps
-// its kind in the first
-__device__ __forceinline__ void split3(float x, uint32_t (&p)[3])
+__device__ __forceinline__ void split2(float a, float b, int parts, uint32_t (&p)[3])
 {
-    const uint32_t bits = __float_as_uint(x);
-    if ((bits & 0x7F800000u) == 0x7F800000u) {
-        p[0] = x == x ? bits >> 16 : 0x7FC0u;
-        p[1] = p[2] = 0;
-        return;
+    p[0] = upper_halves(a, b);
+    const float ra = truncated_rest(a), rb = truncated_rest(b);
+    if (parts == 2) {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(ra, rb);
+        p[1] = *reinterpret_cast<const uint32_t *>(&r);
+        p[2] = 0;
+    } else {
+        p[1] = upper_halves(ra, rb);
+        p[2] = upper_halves(truncated_rest(ra), truncated_rest(rb));
     }
-    const float r1 = x - __uint_as_float(bits & 0xFFFF0000u);
-    const uint32_t b1 = __float_as_uint(r1);
-    const float r2 = r1 - __uint_as_float(b1 & 0xFFFF0000u);
-    p[0] = bits >> 16, p[1] = b1 >> 16, p[2] = __float_as_uint(r2) >> 16;
 }
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// bf16 pair (136 + z, 136 + z): from 128 on the last bit of the significand counts one, from 64 to 128 a half
+__device__ __forceinline__ uint32_t offset_pair(int z) { return uint32_t(z >= -8 ? 0x4308 + z : 0x4310 + 2 * z) * 0x10001u; }
 
-// A CTA of 16 warps holds its share of the activations in shared memory as MMA operands and goes through tiles of channels; a
-// tile's K range is shared by `wk` of its warps, and by the `cl` CTAs of a cluster.  Every warp streams 16 channels x 256 codes at a
-// time through a ring of its own (asynchronous copies; nothing but the warp itself waits for them), so the ring keeps going while
-// the partial sums of a finished tile are added up, in a fixed order.
+// A CTA of 16 warps holds its share of the activations in shared memory as MMA operands.  Its work is a list of units, 16 channels x 256 codes,
+// tile after tile of 16 channels, and every warp takes an equal run of that list: whole tiles, and the end of one and the start of
+// another.  So no warp waits for another until all of them are done, whatever the number of channels and inputs (one tile at a time, K shared by
+// the warps and their sums joined behind each: 57.4 us for 1 x 8192 -> 28672 instead of XX).  A tile's sum is then put together from the runs that
+// it lies in, in their order.  K may also be shared by the `cl` CTAs of a cluster, which read one another's sums.
+// Every warp streams its units through a ring of its own (asynchronous copies; nothing but the warp itself waits for them).
 //
 // Codes of one channel that share 16 bytes are handed to the four lanes of a row by ldmatrix, eight each; a lane's eight give the
 // pairs (0, 4), (1, 5), (2, 6), (3, 7) by shifting, which is the order that the activations are laid out in: any order of K will
@@ -350,99 +359,128 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 {
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int cl = prm.cl, wk = prm.wk, wn = kWarps / wk;
-    const int rank = cl > 1 ? int(blockIdx.x) % cl : 0, cluster = int(blockIdx.x) / cl;
+    const int cl = prm.cl, rank = cl > 1 ? int(blockIdx.x) % cl : 0, cluster = int(blockIdx.x) / cl;
     const int m0 = int(blockIdx.y) * prm.rows, rows = min(prm.rows, prm.M - m0);
-    const int my_k = warp & (wk - 1), my_n = warp >> prm.wk_shift;
-    // this CTA's units, and this warp's
-    const int c_u0 = rank * prm.units_cta, c_u1 = min(prm.units, c_u0 + prm.units_cta);
-    const int u0 = min(c_u1, c_u0 + my_k * prm.units_warp), u1 = min(c_u1, u0 + prm.units_warp);
+    const uint32_t sm0 = smem_addr(smem), ring = sm0 + warp * prm.stages * prm.stage_bytes;
+    const int u_first = rank * prm.units_cta, U = max(0, min(prm.units - u_first, prm.units_cta));   // this CTA's units of a tile
+    const int t_first = int(int64_t(cluster) * prm.tiles / prm.clusters), t_last = int((int64_t(cluster) + 1) * prm.tiles / prm.clusters);
 
-    const uint32_t ring = smem_addr(smem) + warp * prm.stages * prm.stage_bytes;
-
-    // ---- the ring: copies of the unit (pt, pu), one stage after the other
-    int64_t pt = cluster;
-    int pu = u0;
-    if (u0 >= u1) pt = prm.tiles;
-    const int wr = lane >> 3, wc = lane & 7;             // this lane's 16-byte pieces: rows wr, wr + 4, ..
-    auto issue = [&](int slot) {
-        if (pt < prm.tiles) {
-            const uint32_t dst = ring + slot * prm.stage_bytes;
-            const int64_t n0 = (pt * wn + my_n) * kTileN;
-            const int64_t off = int64_t(pu) * (kUnitK / 2) + wc * 16;
-            const int bytes = int(max(int64_t(0), min(int64_t(16), prm.row_bytes - off)));
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int r = wr + 4 * i;
-                const bool in = n0 + r < prm.N && bytes > 0;
-                copy16(dst + r * 128 + ((wc ^ (r & 7)) << 4), in ? prm.W4 + (n0 + r) * prm.ldw + off : prm.W4, in ? bytes : 0);
-            }
-            const int64_t g0 = GB > 1 ? int64_t(pu) * GB : int64_t(pu) * kUnitK / prm.group;
-            const int pieces = prm.s_bytes;              // 16-byte pieces of 16 channels' scales: 4 (fp32) or 2 (bf16)
-            if (lane < GB * pieces) {
-                const int gi = lane / pieces, pc = lane % pieces, per = 16 / prm.s_bytes;
-                const int64_t left = (prm.N - n0 - pc * per) * prm.s_bytes;
-                const bool in = g0 + gi < prm.groups && left > 0;
-                copy16(dst + kUnitBytes + lane * 16, in ? prm.s + (g0 + gi) * prm.lds + (n0 + pc * per) * prm.s_bytes : prm.s,
-                       in ? int(min(int64_t(16), left)) : 0);
-            }
-            if (prm.z && lane < GB) {
-                const bool in = g0 + lane < prm.groups && n0 < prm.N;
-                copy16(dst + prm.z_off + lane * 16, in ? prm.z + (g0 + lane) * prm.ldz + n0 : prm.z,
-                       in ? int(min(int64_t(16), prm.N - n0)) : 0);
-            }
-            if (++pu == u1) pu = u0, pt += prm.clusters;
-        }
-        copies_commit();
-    };
-    for (int i = 0; i < prm.stages - 1; i++) issue(i);
-
-    // ---- activations: per 32 inputs, [column][32 bf16] with each eight as (0, 4), (1, 5), (2, 6), (3, 7); zero behind the last
-    // input, so that whatever lies there in a row of codes counts for nothing
-    const int eights = (c_u1 - c_u0) * (kUnitK / 8);
-    for (int i = tid; i < eights * rows; i += kWarps * 32) {
-        const int m = i / eights, e = i - m * eights;
-        const int64_t k = int64_t(c_u0) * kUnitK + e * 8;
-        float x[8];
-        if (prm.x_f32) load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
-        else load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
-        uint32_t w[3][4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            uint32_t a[3], b[3];
-            split3(act1(x[j], prm.act), a);
-            split3(act1(x[j + 4], prm.act), b);
-#pragma unroll
-            for (int p = 0; p < 3; p++) w[p][j] = a[p] | b[p] << 16;
-        }
-        uint8_t *dst = smem + prm.x_off + size_t(e >> 2) * (prm.cols * 64) + (e & 3) * 16;
-#pragma unroll
-        for (int p = 0; p < 3; p++)
-            if (p < prm.parts) *reinterpret_cast<uint4 *>(dst + (p * prm.rows + m) * 64) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
-    }
-    __syncthreads();
-
-    // ---- tiles
+    const int wr = lane >> 3, wc = lane & 7;             // this lane's 16-byte pieces of a unit: rows wr, wr + 4, ..
+    const uint32_t d0 = wr * 128 + ((wc ^ wr) << 4), d1 = (wr + 4) * 128 + ((wc ^ wr ^ 4) << 4);
+    const int64_t row4 = 4 * prm.ldw;
+    const int pieces = prm.s_bytes, s_group = lane / pieces, s_piece = lane % pieces, s_n = s_piece * (16 / prm.s_bytes);
+    const uint32_t lm_row = (lane & 15) * 128, lm_seg = lane >> 4, lm_x = lane & 7;      // ldmatrix: rows 0-15 of two pieces
     uint32_t xb[NT];                                     // this lane's activations: column g (+ 8 per MMA), codes 8 t ..
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++) xb[nt] = smem_addr(smem) + prm.x_off + min(g + 8 * nt, prm.cols - 1) * 64 + t * 16;
-    const uint32_t lm_row = (lane & 15) * 128, lm_seg = lane >> 4, lm_x = lane & 7;      // ldmatrix: rows 0-15 of two pieces
-    int slot = 0, buf = 0;
-    for (int64_t tile = cluster; tile < prm.tiles; tile += prm.clusters) {
+    for (int nt = 0; nt < NT; nt++) xb[nt] = sm0 + prm.x_off + min(g + 8 * nt, prm.cols - 1) * 64 + t * 16;
+    const uint32_t x_piece = prm.cols * 64;
+
+    for (int t0 = t_first; t0 < t_last; t0 += prm.tiles_round) {
+        const int nt_round = min(prm.tiles_round, t_last - t0);
+        // this warp's run of the list
+        const int total = nt_round * U, begin = int(int64_t(warp) * total / kWarps), end = int((int64_t(warp) + 1) * total / kWarps);
+
+        // ---- the ring: copies of unit (pt, pu), one stage after the other
+        int left = end - begin, pt = 0, pu = 0;
+        if (left > 0) pt = begin / U, pu = begin - pt * U;
+        const uint8_t *src = nullptr, *s_src = nullptr, *z_src = nullptr;
+        int n0 = 0;
+        auto new_tile = [&]() {
+            n0 = (t0 + pt) * kTileN;
+            src = prm.W4 + int64_t(n0 + wr) * prm.ldw + wc * 16;
+            s_src = prm.s + int64_t(n0 + s_n) * prm.s_bytes;
+            z_src = reinterpret_cast<const uint8_t *>(prm.z) + n0;
+        };
+        if (left > 0) new_tile();
+        auto issue = [&](int slot) {
+            if (left > 0) {
+                const uint32_t dst = ring + slot * prm.stage_bytes;
+                const int unit = u_first + pu, off = unit * (kUnitK / 2);
+                const int bytes = max(0, min(16, prm.row_bytes - off - wc * 16));
+                const uint8_t *p = src + off;
+                if (n0 + kTileN <= prm.N && (unit + 1) * (kUnitK / 2) <= prm.row_bytes) {
+                    copy16(dst + d0, p, 16);
+                    copy16(dst + d1, p + row4, 16);
+                    copy16(dst + d0 + 1024, p + 2 * row4, 16);
+                    copy16(dst + d1 + 1024, p + 3 * row4, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bool in = n0 + wr + 4 * i < prm.N && bytes > 0;
+                        copy16(dst + (i & 1 ? d1 : d0) + (i >> 1) * 1024, in ? p + i * row4 : prm.W4, in ? bytes : 0);
+                    }
+                }
+                const int g0 = GB > 1 ? unit * GB : unit / prm.units_group;
+                if (lane < GB * pieces) {                // 16-byte pieces of 16 channels' scales: 4 (fp32) or 2 (bf16)
+                    const int rest = (prm.N - n0 - s_n) * prm.s_bytes;
+                    const bool in = g0 + s_group < prm.groups && rest > 0;
+                    copy16(dst + kUnitBytes + lane * 16, in ? s_src + (g0 + s_group) * prm.lds : prm.s, in ? min(16, rest) : 0);
+                }
+                if (prm.z && lane < GB) {
+                    const bool in = g0 + lane < prm.groups;
+                    copy16(dst + prm.z_off + lane * 16, in ? z_src + (g0 + lane) * prm.ldz : reinterpret_cast<const uint8_t *>(prm.z),
+                           in ? min(16, prm.N - n0) : 0);
+                }
+                left--;
+                if (++pu == U) {
+                    pu = 0, pt++;
+                    if (left > 0) new_tile();
+                }
+            }
+            copies_commit();
+        };
+        for (int i = 0; i < prm.stages - 1; i++) issue(i);
+
+        // ---- activations (once): per 32 inputs, [column][32 bf16] with each eight as (0, 4), (1, 5), (2, 6), (3, 7); zero behind the last
+        // input, so that whatever lies there in a row of codes counts for nothing
+        if (t0 == t_first) {
+            const int eights = U * (kUnitK / 8);
+            for (int i = tid; i < eights * rows; i += kWarps * 32) {
+                const int m = rows == 1 ? 0 : i / eights, e = i - m * eights, k = u_first * kUnitK + e * 8;
+                uint8_t *dst = smem + prm.x_off + size_t(e >> 2) * x_piece + (e & 3) * 16 + m * 64;
+                if (prm.parts == 1 && prm.x_wide && k + 8 <= prm.K) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx + k));
+                    *reinterpret_cast<uint4 *>(dst) = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
+                                                                 __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+                    continue;
+                }
+                float x[8];
+                if (prm.x_f32) load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
+                else load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
+                uint32_t w[3][4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    if (prm.act != SQ_ACT_NONE) unpack2(prm.act == SQ_ACT_SILU ? silu2(x[j], x[j + 4]) : gelu2(x[j], x[j + 4]), x[j], x[j + 4]);
+                    uint32_t p[3];
+                    split2(x[j], x[j + 4], prm.parts, p);
+                    w[0][j] = p[0], w[1][j] = p[1], w[2][j] = p[2];
+                }
+#pragma unroll
+                for (int p = 0; p < 3; p++)
+                    if (p < prm.parts) *reinterpret_cast<uint4 *>(dst + p * prm.rows * 64) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+            }
+            __syncthreads();
+        }
+
+        // ---- the run
+        float *red = reinterpret_cast<float *>(smem + prm.red_off), *head = reinterpret_cast<float *>(smem + prm.head_off);
+        int slot = 0, tile = 0, u = 0;
+        if (end > begin) tile = begin / U, u = begin - tile * U;
+        float *to = u == 0 ? red + tile * (prm.cols * kRedPitch) : head + warp * (prm.cols * kRedPitch);
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int i = 0; i < 4; i++) acc[nt][i] = 0.0f;
-        for (int u = u0; u < u1; u++) {
+        for (int i = begin; i < end; i++) {
             if (prm.stages == 4) copies_wait<2>();
             else if (prm.stages == 3) copies_wait<1>();
             else copies_wait<0>();
             __syncwarp();
             issue(slot == 0 ? prm.stages - 1 : slot - 1);   // the stage that was used up last
             const uint32_t st = ring + slot * prm.stage_bytes;
-            const uint8_t *stp = smem + (st - smem_addr(smem));
-            const uint32_t x_unit = uint32_t(u - c_u0) * 8 * (prm.cols * 64);
+            const uint8_t *stp = smem + (st - sm0);
+            const uint32_t x_unit = uint32_t(u) * 8 * x_piece;
             constexpr int SEGS = 8 / GB;                 // 32-code pieces per group
             uint32_t w[4];
 #pragma unroll
@@ -451,14 +489,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) sum[nt][i] = 0.0f;
+                    for (int j = 0; j < 4; j++) sum[nt][j] = 0.0f;
                 uint32_t off0 = 0x43084308u, off1 = 0x43084308u;          // 136, 136
                 if (prm.z) {
                     const int8_t *z = reinterpret_cast<const int8_t *>(stp + prm.z_off) + gi * 16;
-                    const __nv_bfloat162 z0 = __float2bfloat162_rn(136.0f + float(z[g]));
-                    const __nv_bfloat162 z1 = __float2bfloat162_rn(136.0f + float(z[g + 8]));
-                    off0 = *reinterpret_cast<const uint32_t *>(&z0);
-                    off1 = *reinterpret_cast<const uint32_t *>(&z1);
+                    off0 = offset_pair(z[g]), off1 = offset_pair(z[g + 8]);
                 }
 #pragma unroll
                 for (int s = gi * SEGS; s < (gi + 1) * SEGS; s++) {
@@ -466,12 +501,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                     const uint32_t w0 = w[s % 2 * 2], w1 = w[s % 2 * 2 + 1];
                     uint32_t a[4], b[4];
 #pragma unroll
-                    for (int i = 0; i < 4; i++) a[i] = code_pair(w0, i, off0), b[i] = code_pair(w1, i, off1);
+                    for (int j = 0; j < 4; j++) a[j] = code_pair(w0, j, off0), b[j] = code_pair(w1, j, off1);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         uint32_t x0, x1, x2, x3;
                         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x0), "=r"(x1), "=r"(x2), "=r"(x3)
-                                     : "r"(xb[nt] + x_unit + s * (prm.cols * 64)));
+                                     : "r"(xb[nt] + x_unit + s * x_piece));
                         mma(sum[nt], a[0], b[0], a[1], b[1], x0, x1);
                         mma(sum[nt], a[2], b[2], a[3], b[3], x2, x3);
                     }
@@ -491,57 +526,53 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 }
             }
             slot = slot + 1 == prm.stages ? 0 : slot + 1;
-        }
-        // partial sums of this warp: [column][16 channels]
-        float *red = reinterpret_cast<float *>(smem + prm.red_off + buf * prm.red_bytes);
-        float *mine = red + warp * (prm.cols * kRedPitch);
+            if (++u == U || i + 1 == end) {              // what this run has of the tile: [column][16 channels]
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
+                for (int nt = 0; nt < NT; nt++) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int col = nt * 8 + 2 * t + (i & 1);
-                if (col < prm.cols) mine[col * kRedPitch + g + (i >> 1) * 8] = acc[nt][i];
+                    for (int j = 0; j < 4; j++) {
+                        const int col = nt * 8 + 2 * t + (j & 1);
+                        if (col < prm.cols) to[col * kRedPitch + g + (j >> 1) * 8] = acc[nt][j];
+                        acc[nt][j] = 0.0f;
+                    }
+                }
+                u = 0, tile++;
+                to = red + tile * (prm.cols * kRedPitch);
             }
         }
-        if (cl > 1) {
-            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        } else {
-            __syncthreads();
-        }
-        // output o of the tile, summed by wk lanes: every lane adds a warp's columns over the cluster's CTAs and the parts of an
-        // activation, then the lanes add up; the CTAs of a cluster take turns with the outputs
-        const int outs = kTileN * wn * rows, turns = (outs + cl - 1) / cl;
-        for (int i = tid; i - lane < turns * wk; i += kWarps * 32) {
-            const int o = (i >> prm.wk_shift) * cl + rank, j = i & (wk - 1);
-            float v = 0.0f;
-            if (o < outs) {
-                const int c = o & 15, q = o >> 4, m = q / wn, n16 = q - m * wn;
-                const uint32_t at = smem_addr(red + (n16 * wk + j) * (prm.cols * kRedPitch) + m * kRedPitch + c);
-                for (int r = 0; r < cl; r++) {
-                    uint32_t src = at;
-                    if (cl > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(src) : "r"(at), "r"(r));
+        if (cl > 1) cluster_barrier();
+        else __syncthreads();
+
+        // ---- outputs: the CTAs of a cluster take turns; every sum runs over ranks, runs and the terms of an activation in this order
+        const int outs = nt_round * kTileN * rows;
+        for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
+            const int c = o & 15, q = o >> 4, tl = rows == 1 ? q : q / rows, m = q - tl * rows, n = (t0 + tl) * kTileN + c;
+            if (n >= prm.N) continue;
+            float v = prm.bias ? __ldg(prm.bias + n) : 0.0f;
+            for (int r = 0; r < cl; r++) {
+                const int Ur = min(prm.units - r * prm.units_cta, prm.units_cta), sum_units = nt_round * Ur;
+                if (Ur <= 0) break;
+                // the runs that units tl Ur .. tl Ur + Ur - 1 lie in
+                const int w_first = ((tl * Ur + 1) * kWarps - 1) / sum_units, w_last = ((tl * Ur + Ur) * kWarps - 1) / sum_units;
+                for (int w = w_first; w <= w_last; w++) {
+                    if (w * sum_units / kWarps == (w + 1) * sum_units / kWarps) continue;     // a run of nothing (fewer units than warps)
+                    const float *from = (w == w_first ? red + tl * (prm.cols * kRedPitch) : head + w * (prm.cols * kRedPitch)) + m * kRedPitch + c;
+                    uint32_t at = smem_addr(from);
+                    if (cl > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(r));
                     for (int p = 0; p < prm.parts; p++) {
                         float f;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(src + p * prm.rows * kRedPitch * 4) : "memory");
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at + p * prm.rows * kRedPitch * 4) : "memory");
                         v += f;
                     }
                 }
             }
-            for (int d = 1; d < wk; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-            if (o < outs && j == 0) {
-                const int c = o & 15, q = o >> 4, m = q / wn, n16 = q - m * wn;
-                const int64_t n = (tile * wn + n16) * kTileN + c;
-                if (n < prm.N) {
-                    if (prm.bias) v += __ldg(prm.bias + n);
-                    const int64_t at = (m0 + m) * prm.ldy + n;
-                    if (prm.y_f32) static_cast<float *>(prm.Y)[at] = v;
-                    else static_cast<__nv_bfloat16 *>(prm.Y)[at] = __float2bfloat16_rn(v);
-                }
-            }
+            const int64_t at = (m0 + m) * prm.ldy + n;
+            if (prm.y_f32) static_cast<float *>(prm.Y)[at] = v;
+            else static_cast<__nv_bfloat16 *>(prm.Y)[at] = __float2bfloat16_rn(v);
         }
-        buf ^= 1;            // the next tile's partial sums: whoever still reads these has not passed that tile's barrier
+        if (cl > 1) cluster_barrier();                   // nobody leaves, or writes new sums, while others read these
+        else if (t0 + prm.tiles_round < t_last) __syncthreads();
     }
-    if (cl > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -606,28 +637,27 @@ sq_status matvec_device(MatvecDevice *out)
     return SQ_OK;
 }
 
-std::atomic<int> g_w4_cl{0}, g_w4_wk{0};
-
-// Shared memory of a split, and whether it fits.
-bool lay_out(MatvecParams &p, int gb)
+// Shared memory of a split, and whether it fits: ring, activations, sums of as many tiles as there is room for (at most `tiles`).
+bool lay_out(MatvecParams &p, int gb, int tiles)
 {
     const uint32_t s_bytes = uint32_t(gb * kTileN * p.s_bytes), z_bytes = p.z ? uint32_t(gb * kTileN) : 0u;
     p.z_off = kUnitBytes + s_bytes;
     p.stage_bytes = (p.z_off + z_bytes + 127u) & ~127u;
-    const size_t x_bytes = size_t(p.units_cta) * 8 * p.cols * 64;
-    p.red_bytes = uint32_t(kWarps * p.cols * kRedPitch * 4);
+    const size_t x_bytes = size_t(p.units_cta) * 8 * p.cols * 64, sum = size_t(p.cols) * kRedPitch * 4;
     for (p.stages = kMaxStages; p.stages >= 2; p.stages--) {
+        const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + kWarps * sum;
+        if (fixed + std::min(tiles, 4) * sum > kMaxSmem) continue;
         p.x_off = uint32_t(kWarps * p.stages) * p.stage_bytes;
-        if (p.x_off + x_bytes + 2 * size_t(p.red_bytes) > kMaxSmem) continue;
-        p.red_off = uint32_t(p.x_off + x_bytes);
+        p.head_off = uint32_t(p.x_off + x_bytes);
+        p.red_off = uint32_t(p.head_off + kWarps * sum);
+        p.tiles_round = int(std::min<size_t>(tiles, (kMaxSmem - fixed) / sum));
         return true;
     }
     return false;
 }
+size_t smem_bytes(const MatvecParams &p) { return p.red_off + size_t(p.tiles_round) * p.cols * kRedPitch * 4; }
 
 }  // namespace
-
-void set_w4_tuning(int cl, int wk) { g_w4_cl = cl; g_w4_wk = wk; }
 
 sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
 {
@@ -635,17 +665,21 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     sq_status r = matvec_device(&dev);
     if (r != SQ_OK) return r;
     MatvecParams p{};
-    p.X = a.X; p.ldx = a.ldx; p.M = int(a.M); p.K = a.K; p.x_f32 = a.dt == SQ_F32;
+    p.X = a.X; p.ldx = a.ldx; p.M = int(a.M); p.K = int(a.K); p.x_f32 = a.dt == SQ_F32;
     p.x_wide = aligned16(a.X) && (a.M == 1 || a.ldx * (p.x_f32 ? 4 : 2) % 16 == 0);
     p.act = int(a.act);
-    p.parts = p.x_f32 || p.act != SQ_ACT_NONE ? 3 : 1;
-    p.W4 = static_cast<const uint8_t *>(a.W4); p.ldw = a.ldw; p.N = a.N; p.row_bytes = (a.K + 1) / 2;
-    p.group = int(std::min<int64_t>(a.group, 1 << 30)); p.groups = (a.K + a.group - 1) / a.group;
+    p.y_f32 = a.y_dtype == SQ_F32;
+    p.parts = !p.x_f32 && p.act == SQ_ACT_NONE ? 1 : p.y_f32 ? 3 : 2;
+    p.W4 = static_cast<const uint8_t *>(a.W4); p.ldw = a.ldw; p.N = int(a.N); p.row_bytes = int((a.K + 1) / 2);
+    const int64_t group = std::min<int64_t>(a.group, (a.K + kUnitK - 1) / kUnitK * kUnitK);
+    const int gb = group >= kUnitK ? 1 : int(kUnitK / group);
+    p.units_group = gb > 1 ? 1 : int(group / kUnitK);
+    p.groups = int((a.K + a.group - 1) / a.group);
     p.s = static_cast<const uint8_t *>(a.s); p.s_bytes = a.s_dtype == SQ_F32 ? 4 : 2; p.lds = a.lds * p.s_bytes;
     p.z = a.z; p.ldz = a.ldz; p.bias = a.bias;
-    p.Y = a.Y; p.y_f32 = a.y_dtype == SQ_F32; p.ldy = a.ldy;
+    p.Y = a.Y; p.ldy = a.ldy;
     p.units = int((a.K + kUnitK - 1) / kUnitK);
-    const int gb = a.group >= kUnitK ? 1 : int(kUnitK / a.group);
+    p.tiles = int((a.N + kTileN - 1) / kTileN);
 
     // Rows of a pass: as many as 32 columns take, spread evenly; fewer where the activations would not fit.
     const int most = kMaxCols / p.parts;
@@ -655,23 +689,15 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     for (;; passes++) {
         p.rows = (p.M + passes - 1) / passes;
         p.cols = p.rows * p.parts;
-        const int want_cl = g_w4_cl.load(std::memory_order_relaxed), want_wk = g_w4_wk.load(std::memory_order_relaxed);
         for (int ci = 0; ci < 4; ci++) {
-            for (int wi = 0; wi < 5; wi++) {
-                MatvecParams q = p;
-                q.cl = 1 << ci; q.wk = 1 << wi; q.wk_shift = wi;
-                if ((want_cl && q.cl != want_cl) || (want_wk && q.wk != want_wk)) continue;
-                if (dev.clusters[ci] < 1 || (ci && q.cl > q.units)) continue;
-                q.units_cta = (q.units + q.cl - 1) / q.cl;
-                q.units_warp = (q.units_cta + q.wk - 1) / q.wk;
-                const int tile_n = kTileN * (kWarps / q.wk);
-                q.tiles = (q.N + tile_n - 1) / tile_n;
-                if (!lay_out(q, gb)) continue;
-                q.clusters = int(std::min<int64_t>(q.tiles, dev.clusters[ci]));
-                const double rounds = double((q.tiles + q.clusters - 1) / q.clusters);
-                const double cost = rounds * (0.5 * q.units_warp + (ci ? 1.0 : 0.3)) + 0.0005 * q.cols * q.units_cta * kUnitK / 16.0;
-                if (best == 0 || cost < best) best = cost, pick = q;
-            }
+            p.cl = 1 << ci;
+            if (dev.clusters[ci] < 1 || (ci && p.cl > p.units)) continue;
+            p.units_cta = (p.units + p.cl - 1) / p.cl;
+            p.clusters = std::min(p.tiles, dev.clusters[ci]);
+            const int tiles = (p.tiles + p.clusters - 1) / p.clusters;
+            if (!lay_out(p, gb, tiles)) continue;
+            const double cost = 0.055 * tiles * p.units_cta + (ci ? 0.6 : 0.0) + (p.parts == 1 ? 0.0008 : 0.003) * p.rows * p.units_cta;
+            if (best == 0 || cost < best) best = cost, pick = p;
         }
         if (best != 0) break;
         if (p.rows == 1) return SQ_ERR_UNSUPPORTED;
@@ -679,7 +705,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(pick.clusters * pick.cl), unsigned((pick.M + pick.rows - 1) / pick.rows));
     cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = pick.red_off + 2 * pick.red_bytes;
+    cfg.dynamicSmemBytes = smem_bytes(pick);
     cfg.stream = st;
     cudaLaunchAttribute at{};
     if (pick.cl > 1) {

@@ -7,7 +7,8 @@ Tolerance of the product.  Codes, zero-points and the bf16 terms of an activatio
 the sum of magnitudes, and a group (at most 256 inputs at a time) takes group / 16 of them: 1.0625 * group * 2^-23.  Scales, sums
 over groups, warps, CTAs and the three terms of an fp32 value, and the bias: one rounding of 2^-24 each, of partial sums that are no
 larger than the sum of magnitudes.  The third term of an fp32 value ends at bf16's smallest subnormal, 2^-133, and sums of subnormals are rounded at
-2^-149.  The activation functions come with the errors that the C header gives.  bf16 outputs are rounded once more, by
+2^-149.  The activation functions come with the errors that the C header gives, and
+behind bf16 outputs values that are no bf16 numbers are rounded to 2^-17 of their size.  bf16 outputs are rounded once more, by
 at most half a step (2^-8)."""
 import numpy as np
 import pytest
@@ -153,6 +154,8 @@ def check_product(Y, X, W, bias, act, G, K):
         want, mags = want + bias.double(), mags + bias.double().abs()
     roundings = 1.0625 * min(G, 256) * 2 + 2 * (-(-K // min(G, 256))) + 8 * 16 * 3 + 2
     tol = roundings * 2.0 ** -24 * mags + of_act
+    if Y.dtype == BF and (X.dtype == F32 or act):
+        tol = tol + 2.0 ** -17 * (a.abs() @ W.abs().t())
     if Y.dtype == BF:
         tol = tol + 2.0 ** -8 * (want.abs() + tol)
     err = (Y.double() - want).abs()
