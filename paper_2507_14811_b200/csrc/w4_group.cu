@@ -3,11 +3,13 @@
 //
 //   w'[n][k] = (c[n][k] - z[g][n]) s[g][n],  g = k / group          y[m][n] = sum_g s[g][n] sum_{k in g} (c - z) a(x[m][k]) + b[n]
 //
-// The product is bound by reading the codes once: N K / 2 bytes, 12.8 T codes a second at copy bandwidth, for which 148 SMs have
-// 2.8 lane instructions per code.  Converting a code to fp32 and one FMA per row would take more than that for a single row;
-// so the codes go to the tensor cores as bf16 integers (1.5 instructions per code whatever the number of rows, up to 8):
-// mma.m16n8k16 with 16 channels on its rows and the activations' rows on its 8 columns.  tcgen05 would want the expanded codes in
-// shared memory, four times the bytes that came in; the tensor pipe is far from being a bound here.
+// The product is bound by reading the codes once: N K / 2 bytes, 12.8 T codes a second at copy bandwidth.  That leaves 148 SMs 2.8 lane
+// instructions per code, and half of that on either arithmetic pipe, so codes are not turned into real numbers one by one.  A byte of two
+// codes is two signed bytes 16 c after one mask each (0.4 instructions per code), which integer matrix instructions take as they are:
+// mma.m16n8k32, 16 channels on its rows.  The activations become 23-bit fixed-point numbers of their group's range, as three signed
+// bytes in three of its 8 columns; products and a group's sums are exact integers, and scales and zero-points come in behind a group.
+// (Expanded to bf16 instead, 1.4 instructions per code, the same design took 38.3 us for 1 x 8192 -> 28672 with zero-points.)  tcgen05
+// would want the expanded codes in shared memory, twice the bytes that came in, and has nothing to offer: the tensor pipe is no bound here.
 #include <cuda_bf16.h>
 #include <algorithm>
 #include <atomic>
@@ -255,19 +257,21 @@ constexpr int kUnitK = 256;          // codes per channel and ring stage: 128 by
 constexpr int kUnitBytes = kTileN * kUnitK / 2;
 constexpr int kMaxStages = 4;        // of a warp's ring; 2 or 3 where the activations leave no room for more
 constexpr int kRedPitch = 20;        // floats per column of a tile's sums (16 used; 20 keeps the stores off one bank)
-constexpr int kMaxCols = 32;
+constexpr int kMaxCols = 48;         // columns of a pass: 16 rows of three bytes each
+constexpr int kMaxBlock = 128;       // inputs that share a fixed-point range: a group, or this many of a longer one
 
 struct MatvecParams {
     const void *X;
     int64_t ldx;
     int M, rows;                     // rows of X, rows of one pass (grid.y)
     int K;
-    int x_f32, x_wide, act, parts;   // parts: bf16 terms per activation
+    int x_f32, x_wide, act;
+    int block;                       // inputs of a fixed-point range: 32, 64 or 128
     const uint8_t *W4;
     int64_t ldw;
     int N, row_bytes;
-    int units_group;                 // units of a long group (short ones: 1)
-    int groups;
+    int groups, unit_groups;         // in all; of a unit (at least 1)
+    int units_group;                 // units of a group (at least 1)
     const uint8_t *s;
     int s_bytes;                     // 4 or 2
     int64_t lds;                     // bytes
@@ -281,9 +285,9 @@ struct MatvecParams {
     int units, units_cta;            // of K, of a CTA
     int tiles, clusters;
     int tiles_round;                 // tiles whose sums fit in shared memory
-    int cols;                        // columns in use: rows * parts
+    int cols, cols8;                 // columns in use, 3 * rows; rounded up to whole MMAs
     int stages;
-    uint32_t stage_bytes, z_off, x_off, red_off, head_off;
+    uint32_t stage_bytes, z_off, x_off, f_off, xs_off, red_off, head_off;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -300,60 +304,69 @@ __device__ __forceinline__ void load_matrices(uint32_t addr, uint32_t (&r)[4])
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+// d = a b + c with signed bytes
+__device__ __forceinline__ void mma(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const int (&c)[4])
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
-// Codes i and i + 4 of a word of eight, as bf16 integers less an offset: a nibble c with its top bit flipped is c + 8, and the
-// bits 0x4300 | (c + 8) are the bf16 number 136 + c, so that subtracting 136 + z leaves c - z, exactly.
-__device__ __forceinline__ uint32_t code_pair(uint32_t word, int i, uint32_t offset)
+__device__ __forceinline__ uint32_t shared_u32(uint32_t at)
 {
-    uint32_t v, d;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(v) : "r"(word >> (4 * i)), "r"(0x000F000Fu), "r"(0x43084308u));   // (a & b) ^ c
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(v), "r"(offset));
-    return d;
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
 }
-// Two activations as sums of bf16 terms: truncations of 8 significant bits each, three of which hold an fp32 value exactly (down to
-// 2^-133, where bf16 ends), or a truncation and a rounded rest, 2^-17 of the value off, which is taken where the output is bf16.  What is
-// infinite keeps to the first term; a NaN is one in all.
-__device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
-__device__ __forceinline__ float truncated_rest(float x)
+__device__ __forceinline__ uint32_t shared_u16(uint32_t at)
 {
-    const float r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-    return fabsf(x) == __int_as_float(0x7F800000) ? 0.0f : r;
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+    return v;
 }
-__device__ __forceinline__ void split2(float a, float b, int parts, uint32_t (&p)[3])
+__device__ __forceinline__ int shared_s8(uint32_t at)
 {
-    p[0] = upper_halves(a, b);
-    const float ra = truncated_rest(a), rb = truncated_rest(b);
-    if (parts == 2) {
-        const __nv_bfloat162 r = __floats2bfloat162_rn(ra, rb);
-        p[1] = *reinterpret_cast<const uint32_t *>(&r);
-        p[2] = 0;
-    } else {
-        p[1] = upper_halves(ra, rb);
-        p[2] = upper_halves(truncated_rest(ra), truncated_rest(rb));
-    }
+    int v;
+    asm volatile("ld.shared.s8 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint4 shared_v4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 shared_v2(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+// bytes `which` of four words
+__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t which)
+{
+    return __byte_perm(__byte_perm(a, b, which | (which + 4) << 4), __byte_perm(c, d, which | (which + 4) << 4), 0x5410);
 }
 __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// bf16 pair (136 + z, 136 + z): from 128 on the last bit of the significand counts one, from 64 to 128 a half
-__device__ __forceinline__ uint32_t offset_pair(int z) { return uint32_t(z >= -8 ? 0x4308 + z : 0x4310 + 2 * z) * 0x10001u; }
-
 // A CTA of 16 warps holds its share of the activations in shared memory as MMA operands.  Its work is a list of units, 16 channels x 256 codes,
 // tile after tile of 16 channels, and every warp takes an equal run of that list: whole tiles, and the end of one and the start of
 // another.  So no warp waits for another until all of them are done, whatever the number of channels and inputs (one tile at a time, K shared by
-// the warps and their sums joined behind each: 57.4 us for 1 x 8192 -> 28672 instead of XX).  A tile's sum is then put together from the runs that
-// it lies in, in their order.  K may also be shared by the `cl` CTAs of a cluster, which read one another's sums.
+// the warps and their sums joined behind each, took half as long again).  A tile's sum is then put together from the runs that it lies
+// in, in their order.  K may also be shared by the `cl` CTAs of a cluster, which read one another's sums.
 // Every warp streams its units through a ring of its own (asynchronous copies; nothing but the warp itself waits for them).
 //
-// Codes of one channel that share 16 bytes are handed to the four lanes of a row by ldmatrix, eight each; a lane's eight give the
-// pairs (0, 4), (1, 5), (2, 6), (3, 7) by shifting, which is the order that the activations are laid out in: any order of K will
-// do as long as both operands have it.  GB: groups of inputs per ring stage, 256 / group (1 for longer groups).  Products of codes
-// and bf16 activations are exact, a group's sum is fp32, and the scale is applied to it in fp32.
+// Codes of one channel that share 16 bytes are handed to the four lanes of a row by ldmatrix, eight each: (w << 4) & 0xF0F0F0F0 are the
+// bytes 16 c of codes 0, 2, 4, 6 and w & 0xF0F0F0F0 those of 1, 3, 5, 7, and the activations are laid out in that order, too; any order
+// of K will do as long as both operands have it.
+//
+// Fixed point: with 2^E <= max|x| < 2^(E+1) over a block of at most 128 inputs, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
+// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact); the bytes of (q + 0x808080) ^ 0x808080 are signed q0, q1, q2 with
+// q = q0 + 256 q1 + 65536 q2.  A block's sum of 16 (c - z) q_i stays within 2^22 for zero-points in [-8, 7], so that it becomes a float by
+// starting at the bits of 1.5 * 2^23 and subtracting that number: the start, less the zero-point times the block's sum of q_i, is the
+// MMA's addend.  Behind it one FMA in fp32 with scale times 2^(E - 25) 256^i.  A block with an infinity or a NaN has the factor NaN.
+// GB: blocks of a unit (2, 4, 8).
 template <int NT, int GB>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_constant__ MatvecParams prm)
 {
@@ -368,12 +381,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
     const int wr = lane >> 3, wc = lane & 7;             // this lane's 16-byte pieces of a unit: rows wr, wr + 4, ..
     const uint32_t d0 = wr * 128 + ((wc ^ wr) << 4), d1 = (wr + 4) * 128 + ((wc ^ wr ^ 4) << 4);
     const int64_t row4 = 4 * prm.ldw;
-    const int pieces = prm.s_bytes, s_group = lane / pieces, s_piece = lane % pieces, s_n = s_piece * (16 / prm.s_bytes);
+    const int pieces = prm.s_bytes, s_group = lane / pieces, s_n = lane % pieces * (16 / prm.s_bytes);   // 16-byte pieces of 16 channels' scales
+    const bool s_lane = lane < prm.unit_groups * pieces, z_lane = prm.z && lane < prm.unit_groups;
     const uint32_t lm_row = (lane & 15) * 128, lm_seg = lane >> 4, lm_x = lane & 7;      // ldmatrix: rows 0-15 of two pieces
+    uint32_t lm[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) lm[i] = lm_row + (((2 * i + lm_seg) ^ lm_x) << 4);
     uint32_t xb[NT];                                     // this lane's activations: column g (+ 8 per MMA), codes 8 t ..
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) xb[nt] = sm0 + prm.x_off + min(g + 8 * nt, prm.cols - 1) * 64 + t * 16;
-    const uint32_t x_piece = prm.cols * 64;
+    const uint32_t x_pair = prm.cols * 64;               // 64 codes of all columns
+    const uint32_t s_step = prm.unit_groups == GB ? 16 * prm.s_bytes : 0, z_step = prm.unit_groups == GB ? 16 : 0;
 
     for (int t0 = t_first; t0 < t_last; t0 += prm.tiles_round) {
         const int nt_round = min(prm.tiles_round, t_last - t0);
@@ -388,38 +406,40 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         auto new_tile = [&]() {
             n0 = (t0 + pt) * kTileN;
             src = prm.W4 + int64_t(n0 + wr) * prm.ldw + wc * 16;
-            s_src = prm.s + int64_t(n0 + s_n) * prm.s_bytes;
-            z_src = reinterpret_cast<const uint8_t *>(prm.z) + n0;
+            s_src = prm.s + int64_t(n0 + s_n) * prm.s_bytes + s_group * prm.lds;
+            z_src = reinterpret_cast<const uint8_t *>(prm.z) + n0 + lane * prm.ldz;
         };
         if (left > 0) new_tile();
         auto issue = [&](int slot) {
             if (left > 0) {
                 const uint32_t dst = ring + slot * prm.stage_bytes;
                 const int unit = u_first + pu, off = unit * (kUnitK / 2);
-                const int bytes = max(0, min(16, prm.row_bytes - off - wc * 16));
+                const int g0 = prm.units_group > 1 ? unit / prm.units_group : unit * prm.unit_groups;
                 const uint8_t *p = src + off;
-                if (n0 + kTileN <= prm.N && (unit + 1) * (kUnitK / 2) <= prm.row_bytes) {
+                if (n0 + kTileN <= prm.N && off + kUnitK / 2 <= prm.row_bytes) {
                     copy16(dst + d0, p, 16);
                     copy16(dst + d1, p + row4, 16);
                     copy16(dst + d0 + 1024, p + 2 * row4, 16);
                     copy16(dst + d1 + 1024, p + 3 * row4, 16);
+                    if (s_lane) copy16(dst + kUnitBytes + lane * 16, s_src + g0 * prm.lds, 16);
+                    if (z_lane) copy16(dst + prm.z_off + lane * 16, z_src + g0 * prm.ldz, 16);
                 } else {
+                    const int bytes = max(0, min(16, prm.row_bytes - off - wc * 16));
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         const bool in = n0 + wr + 4 * i < prm.N && bytes > 0;
                         copy16(dst + (i & 1 ? d1 : d0) + (i >> 1) * 1024, in ? p + i * row4 : prm.W4, in ? bytes : 0);
                     }
-                }
-                const int g0 = GB > 1 ? unit * GB : unit / prm.units_group;
-                if (lane < GB * pieces) {                // 16-byte pieces of 16 channels' scales: 4 (fp32) or 2 (bf16)
-                    const int rest = (prm.N - n0 - s_n) * prm.s_bytes;
-                    const bool in = g0 + s_group < prm.groups && rest > 0;
-                    copy16(dst + kUnitBytes + lane * 16, in ? s_src + (g0 + s_group) * prm.lds : prm.s, in ? min(16, rest) : 0);
-                }
-                if (prm.z && lane < GB) {
-                    const bool in = g0 + lane < prm.groups;
-                    copy16(dst + prm.z_off + lane * 16, in ? z_src + (g0 + lane) * prm.ldz : reinterpret_cast<const uint8_t *>(prm.z),
-                           in ? min(16, prm.N - n0) : 0);
+                    if (s_lane) {
+                        const int rest = (prm.N - n0 - s_n) * prm.s_bytes;
+                        const bool in = g0 + s_group < prm.groups && rest > 0;
+                        copy16(dst + kUnitBytes + lane * 16, in ? s_src + g0 * prm.lds : prm.s, in ? min(16, rest) : 0);
+                    }
+                    if (z_lane) {
+                        const bool in = g0 + lane < prm.groups;
+                        copy16(dst + prm.z_off + lane * 16, in ? z_src + g0 * prm.ldz : reinterpret_cast<const uint8_t *>(prm.z),
+                               in ? min(16, prm.N - n0) : 0);
+                    }
                 }
                 left--;
                 if (++pu == U) {
@@ -431,33 +451,55 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         };
         for (int i = 0; i < prm.stages - 1; i++) issue(i);
 
-        // ---- activations (once): per 32 inputs, [column][32 bf16] with each eight as (0, 4), (1, 5), (2, 6), (3, 7); zero behind the last
-        // input, so that whatever lies there in a row of codes counts for nothing
+        // ---- activations (once): fixed point, a lane takes eight inputs; per 64 inputs [column][four eights][16 bytes], two words for each
+        // half of the 64; zero behind the last input, so that whatever lies there in a row of codes counts for nothing.  Whole warps go
+        // through the loop: the lanes of a block settle on its range by shuffles.
         if (t0 == t_first) {
-            const int eights = U * (kUnitK / 8);
-            for (int i = tid; i < eights * rows; i += kWarps * 32) {
+            const int eights = U * (kUnitK / 8), lanes = prm.block / 8;
+            for (int i = tid; i < eights * rows; i += kWarps * 32) {                    // (a multiple of 32)
                 const int m = rows == 1 ? 0 : i / eights, e = i - m * eights, k = u_first * kUnitK + e * 8;
-                uint8_t *dst = smem + prm.x_off + size_t(e >> 2) * x_piece + (e & 3) * 16 + m * 64;
-                if (prm.parts == 1 && prm.x_wide && k + 8 <= prm.K) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx + k));
-                    *reinterpret_cast<uint4 *>(dst) = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
-                                                                 __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-                    continue;
-                }
                 float x[8];
                 if (prm.x_f32) load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
                 else load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
-                uint32_t w[3][4];
+                if (prm.act != SQ_ACT_NONE) {
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    if (prm.act != SQ_ACT_NONE) unpack2(prm.act == SQ_ACT_SILU ? silu2(x[j], x[j + 4]) : gelu2(x[j], x[j + 4]), x[j], x[j + 4]);
-                    uint32_t p[3];
-                    split2(x[j], x[j + 4], prm.parts, p);
-                    w[0][j] = p[0], w[1][j] = p[1], w[2][j] = p[2];
+                    for (int j = 0; j < 8; j += 2) unpack2(prm.act == SQ_ACT_SILU ? silu2(x[j], x[j + 1]) : gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
                 }
+                uint32_t top = 0;                        // largest magnitude, as bits
 #pragma unroll
-                for (int p = 0; p < 3; p++)
-                    if (p < prm.parts) *reinterpret_cast<uint4 *>(dst + p * prm.rows * 64) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+                for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+                for (int d = 1; d < lanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                const bool finite = top < 0x7F800000u;
+                const uint32_t be = max(top >> 23, 27u);                                // biased E; smaller ranges count as 2^-100
+                const float up = finite ? __uint_as_float((275u - be) << 23) : 0.0f;    // 2^(21 - E)
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    v[j] = (__float_as_uint(finite ? fmaf(x[j], up, kRoundMagic) : kRoundMagic) - (0x4B400000u - 0x808080u)) ^ 0x808080u;
+                uint8_t *dst = smem + prm.x_off + size_t(e >> 3) * x_pair + (e & 3) * 16 + (e >> 2 & 1) * 8;
+                int sum[3];
+#pragma unroll
+                for (int p = 0; p < 3; p++) {
+                    const uint2 b = make_uint2(bytes_of(v[0], v[2], v[4], v[6], p), bytes_of(v[1], v[3], v[5], v[7], p));
+                    *reinterpret_cast<uint2 *>(dst + (p * prm.rows + m) * 64) = b;
+                    sum[p] = __dp4a(int(b.x), 0x01010101, __dp4a(int(b.y), 0x01010101, 0));
+                }
+                if (prm.z) {
+                    for (int d = 1; d < lanes; d <<= 1) {
+#pragma unroll
+                        for (int p = 0; p < 3; p++) sum[p] += __shfl_xor_sync(0xFFFFFFFFu, sum[p], d);
+                    }
+                }
+                if (lane % lanes == 0) {
+                    const int at = (i - m * eights) / lanes * prm.cols8 + m;
+                    float *f = reinterpret_cast<float *>(smem + prm.f_off) + at;
+                    int *xs = reinterpret_cast<int *>(smem + prm.xs_off) + at;
+#pragma unroll
+                    for (int p = 0; p < 3; p++) {
+                        f[p * prm.rows] = finite ? __uint_as_float((be - 25u + 8u * p) << 23) : __uint_as_float(0x7FC00000u);
+                        if (prm.z) xs[p * prm.rows] = 16 * sum[p];
+                    }
+                }
             }
             __syncthreads();
         }
@@ -478,52 +520,62 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             else copies_wait<0>();
             __syncwarp();
             issue(slot == 0 ? prm.stages - 1 : slot - 1);   // the stage that was used up last
-            const uint32_t st = ring + slot * prm.stage_bytes;
-            const uint8_t *stp = smem + (st - sm0);
-            const uint32_t x_unit = uint32_t(u) * 8 * x_piece;
-            constexpr int SEGS = 8 / GB;                 // 32-code pieces per group
-            uint32_t w[4];
-#pragma unroll
-            for (int gi = 0; gi < GB; gi++) {
-                float sum[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) sum[nt][j] = 0.0f;
-                uint32_t off0 = 0x43084308u, off1 = 0x43084308u;          // 136, 136
+            const uint32_t st = ring + slot * prm.stage_bytes, x_unit = uint32_t(u) * 4 * x_pair;
+            const uint32_t f_at = sm0 + prm.f_off + (u * GB * prm.cols8 + 2 * t) * 4;
+            const uint32_t s_at = st + kUnitBytes + g * prm.s_bytes, z_at = st + prm.z_off + g;
+            int sum[NT][4];
+            // the sums of a block start here
+            auto start = [&](int b) {
                 if (prm.z) {
-                    const int8_t *z = reinterpret_cast<const int8_t *>(stp + prm.z_off) + gi * 16;
-                    off0 = offset_pair(z[g]), off1 = offset_pair(z[g + 8]);
-                }
-#pragma unroll
-                for (int s = gi * SEGS; s < (gi + 1) * SEGS; s++) {
-                    if (s % 2 == 0) load_matrices(st + lm_row + (((s + lm_seg) ^ lm_x) << 4), w);
-                    const uint32_t w0 = w[s % 2 * 2], w1 = w[s % 2 * 2 + 1];
-                    uint32_t a[4], b[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) a[j] = code_pair(w0, j, off0), b[j] = code_pair(w1, j, off1);
+                    const int z0 = shared_s8(z_at + b * z_step), z1 = shared_s8(z_at + b * z_step + 8);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
-                        uint32_t x0, x1, x2, x3;
-                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x0), "=r"(x1), "=r"(x2), "=r"(x3)
-                                     : "r"(xb[nt] + x_unit + s * x_piece));
-                        mma(sum[nt], a[0], b[0], a[1], b[1], x0, x1);
-                        mma(sum[nt], a[2], b[2], a[3], b[3], x2, x3);
+                        const uint2 xs = shared_v2(f_at + (prm.xs_off - prm.f_off) + (b * prm.cols8 + nt * 8) * 4);
+                        sum[nt][0] = kMagicBits - z0 * int(xs.x), sum[nt][1] = kMagicBits - z0 * int(xs.y);
+                        sum[nt][2] = kMagicBits - z1 * int(xs.x), sum[nt][3] = kMagicBits - z1 * int(xs.y);
                     }
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int j = 0; j < 4; j++) sum[nt][j] = kMagicBits;
                 }
+            };
+            // .. and end here
+            auto finish = [&](int b) {
                 float s0, s1;
                 if (prm.s_bytes == 4) {
-                    const float *sc = reinterpret_cast<const float *>(stp + kUnitBytes) + gi * 16;
-                    s0 = sc[g], s1 = sc[g + 8];
+                    s0 = __uint_as_float(shared_u32(s_at + b * s_step)), s1 = __uint_as_float(shared_u32(s_at + b * s_step + 32));
                 } else {
-                    const uint16_t *sc = reinterpret_cast<const uint16_t *>(stp + kUnitBytes) + gi * 16;
-                    s0 = __uint_as_float(uint32_t(sc[g]) << 16), s1 = __uint_as_float(uint32_t(sc[g + 8]) << 16);
+                    s0 = __uint_as_float(shared_u16(s_at + b * s_step) << 16), s1 = __uint_as_float(shared_u16(s_at + b * s_step + 16) << 16);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
-                    acc[nt][0] = fmaf(s0, sum[nt][0], acc[nt][0]), acc[nt][1] = fmaf(s0, sum[nt][1], acc[nt][1]);
-                    acc[nt][2] = fmaf(s1, sum[nt][2], acc[nt][2]), acc[nt][3] = fmaf(s1, sum[nt][3], acc[nt][3]);
+                    const uint2 fb = shared_v2(f_at + (b * prm.cols8 + nt * 8) * 4);
+                    const float f0 = __uint_as_float(fb.x), f1 = __uint_as_float(fb.y);
+                    acc[nt][0] = fmaf(s0 * f0, __int_as_float(sum[nt][0]) - kRoundMagic, acc[nt][0]);
+                    acc[nt][1] = fmaf(s0 * f1, __int_as_float(sum[nt][1]) - kRoundMagic, acc[nt][1]);
+                    acc[nt][2] = fmaf(s1 * f0, __int_as_float(sum[nt][2]) - kRoundMagic, acc[nt][2]);
+                    acc[nt][3] = fmaf(s1 * f1, __int_as_float(sum[nt][3]) - kRoundMagic, acc[nt][3]);
                 }
+            };
+#pragma unroll
+            for (int pr = 0; pr < 4; pr++) {             // 64 codes at a time: two pieces of 32
+                uint32_t w[4];
+                load_matrices(st + lm[pr], w);
+                constexpr uint32_t high = 0xF0F0F0F0u;
+                uint4 x[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) x[nt] = shared_v4(xb[nt] + x_unit + pr * x_pair);
+                if (GB == 8 || GB == 4 || pr % 2 == 0) start(GB == 2 ? pr / 2 : GB == 4 ? pr : 2 * pr);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) mma(sum[nt], w[0] << 4 & high, w[1] << 4 & high, w[0] & high, w[1] & high, x[nt].x, x[nt].y, sum[nt]);
+                if (GB == 8) finish(2 * pr), start(2 * pr + 1);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) mma(sum[nt], w[2] << 4 & high, w[3] << 4 & high, w[2] & high, w[3] & high, x[nt].z, x[nt].w, sum[nt]);
+                if (GB == 8) finish(2 * pr + 1);
+                else if (GB == 4) finish(pr);
+                else if (pr % 2 == 1) finish(pr / 2);
             }
             slot = slot + 1 == prm.stages ? 0 : slot + 1;
             if (++u == U || i + 1 == end) {              // what this run has of the tile: [column][16 channels]
@@ -543,7 +595,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         if (cl > 1) cluster_barrier();
         else __syncthreads();
 
-        // ---- outputs: the CTAs of a cluster take turns; every sum runs over ranks, runs and the terms of an activation in this order
+        // ---- outputs: the CTAs of a cluster take turns; every sum runs over ranks, runs and an activation's bytes in this order
         const int outs = nt_round * kTileN * rows;
         for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
             const int c = o & 15, q = o >> 4, tl = rows == 1 ? q : q / rows, m = q - tl * rows, n = (t0 + tl) * kTileN + c;
@@ -559,7 +611,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                     const float *from = (w == w_first ? red + tl * (prm.cols * kRedPitch) : head + w * (prm.cols * kRedPitch)) + m * kRedPitch + c;
                     uint32_t at = smem_addr(from);
                     if (cl > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(r));
-                    for (int p = 0; p < prm.parts; p++) {
+#pragma unroll
+                    for (int p = 0; p < 3; p++) {
                         float f;
                         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at + p * prm.rows * kRedPitch * 4) : "memory");
                         v += f;
@@ -581,19 +634,21 @@ template <int NT>
 const void *matvec_kernel(int gb)
 {
     switch (gb) {
-        case 1: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 1>);
         case 2: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 2>);
         case 4: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 4>);
         default: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 8>);
     }
 }
+constexpr int kMaxNt = kMaxCols / 8;
 const void *matvec_kernel(int nt, int gb)
 {
     switch (nt) {
         case 1: return matvec_kernel<1>(gb);
         case 2: return matvec_kernel<2>(gb);
         case 3: return matvec_kernel<3>(gb);
-        default: return matvec_kernel<4>(gb);
+        case 4: return matvec_kernel<4>(gb);
+        case 5: return matvec_kernel<5>(gb);
+        default: return matvec_kernel<6>(gb);
     }
 }
 
@@ -614,8 +669,8 @@ sq_status matvec_device(MatvecDevice *out)
         if (d.device == dev) { *out = d; return SQ_OK; }
     MatvecDevice d{dev, 0, {0, 0, 0, 0}};
     cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
-    for (int nt = 1; nt <= 4 && e == cudaSuccess; nt++)
-        for (int gb = 1; gb <= 8 && e == cudaSuccess; gb *= 2)
+    for (int nt = 1; nt <= kMaxNt && e == cudaSuccess; nt++)
+        for (int gb = 2; gb <= 8 && e == cudaSuccess; gb *= 2)
             e = cudaFuncSetAttribute(matvec_kernel(nt, gb), cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem));
     d.clusters[0] = d.sms;
     for (int i = 1; i <= 3 && e == cudaSuccess; i++) {
@@ -629,7 +684,7 @@ sq_status matvec_device(MatvecDevice *out)
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 1), &cfg);
+        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 2), &cfg);
     }
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     g_devices.push_back(d);
@@ -637,18 +692,22 @@ sq_status matvec_device(MatvecDevice *out)
     return SQ_OK;
 }
 
-// Shared memory of a split, and whether it fits: ring, activations, sums of as many tiles as there is room for (at most `tiles`).
+// Shared memory of a split, and whether it fits: ring, activations with their blocks' factors (and sums), sums of as many tiles as
+// there is room for (at most `tiles`).
 bool lay_out(MatvecParams &p, int gb, int tiles)
 {
-    const uint32_t s_bytes = uint32_t(gb * kTileN * p.s_bytes), z_bytes = p.z ? uint32_t(gb * kTileN) : 0u;
+    const uint32_t s_bytes = uint32_t(p.unit_groups * kTileN * p.s_bytes), z_bytes = p.z ? uint32_t(p.unit_groups * kTileN) : 0u;
     p.z_off = kUnitBytes + s_bytes;
     p.stage_bytes = (p.z_off + z_bytes + 127u) & ~127u;
-    const size_t x_bytes = size_t(p.units_cta) * 8 * p.cols * 64, sum = size_t(p.cols) * kRedPitch * 4;
+    const size_t x_bytes = size_t(p.units_cta) * 4 * p.cols * 64, f_bytes = size_t(p.units_cta) * gb * p.cols8 * 4;
+    const size_t sum = size_t(p.cols) * kRedPitch * 4;
     for (p.stages = kMaxStages; p.stages >= 2; p.stages--) {
-        const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + kWarps * sum;
+        const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + f_bytes * (p.z ? 2 : 1) + kWarps * sum;
         if (fixed + std::min(tiles, 4) * sum > kMaxSmem) continue;
         p.x_off = uint32_t(kWarps * p.stages) * p.stage_bytes;
-        p.head_off = uint32_t(p.x_off + x_bytes);
+        p.f_off = uint32_t(p.x_off + x_bytes);
+        p.xs_off = uint32_t(p.f_off + (p.z ? f_bytes : 0));
+        p.head_off = uint32_t(p.xs_off + f_bytes);
         p.red_off = uint32_t(p.head_off + kWarps * sum);
         p.tiles_round = int(std::min<size_t>(tiles, (kMaxSmem - fixed) / sum));
         return true;
@@ -669,11 +728,12 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     p.x_wide = aligned16(a.X) && (a.M == 1 || a.ldx * (p.x_f32 ? 4 : 2) % 16 == 0);
     p.act = int(a.act);
     p.y_f32 = a.y_dtype == SQ_F32;
-    p.parts = !p.x_f32 && p.act == SQ_ACT_NONE ? 1 : p.y_f32 ? 3 : 2;
     p.W4 = static_cast<const uint8_t *>(a.W4); p.ldw = a.ldw; p.N = int(a.N); p.row_bytes = int((a.K + 1) / 2);
     const int64_t group = std::min<int64_t>(a.group, (a.K + kUnitK - 1) / kUnitK * kUnitK);
-    const int gb = group >= kUnitK ? 1 : int(kUnitK / group);
-    p.units_group = gb > 1 ? 1 : int(group / kUnitK);
+    p.block = int(std::min<int64_t>(group, kMaxBlock));
+    const int gb = kUnitK / p.block;
+    p.unit_groups = group >= kUnitK ? 1 : int(kUnitK / group);
+    p.units_group = group >= kUnitK ? int(group / kUnitK) : 1;
     p.groups = int((a.K + a.group - 1) / a.group);
     p.s = static_cast<const uint8_t *>(a.s); p.s_bytes = a.s_dtype == SQ_F32 ? 4 : 2; p.lds = a.lds * p.s_bytes;
     p.z = a.z; p.ldz = a.ldz; p.bias = a.bias;
@@ -681,14 +741,15 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     p.units = int((a.K + kUnitK - 1) / kUnitK);
     p.tiles = int((a.N + kTileN - 1) / kTileN);
 
-    // Rows of a pass: as many as 32 columns take, spread evenly; fewer where the activations would not fit.
-    const int most = kMaxCols / p.parts;
+    // Rows of a pass: as many as 48 columns take, spread evenly; fewer where the activations would not fit.
+    const int most = kMaxCols / 3;
     int passes = (p.M + most - 1) / most;
     double best = 0;
     MatvecParams pick{};
     for (;; passes++) {
         p.rows = (p.M + passes - 1) / passes;
-        p.cols = p.rows * p.parts;
+        p.cols = p.rows * 3;
+        p.cols8 = (p.cols + 7) / 8 * 8;
         for (int ci = 0; ci < 4; ci++) {
             p.cl = 1 << ci;
             if (dev.clusters[ci] < 1 || (ci && p.cl > p.units)) continue;
@@ -696,7 +757,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
             p.clusters = std::min(p.tiles, dev.clusters[ci]);
             const int tiles = (p.tiles + p.clusters - 1) / p.clusters;
             if (!lay_out(p, gb, tiles)) continue;
-            const double cost = 0.055 * tiles * p.units_cta + (ci ? 0.6 : 0.0) + (p.parts == 1 ? 0.0008 : 0.003) * p.rows * p.units_cta;
+            const double cost = 0.055 * tiles * p.units_cta + (ci ? 0.6 : 0.0) + 0.003 * p.rows * p.units_cta;
             if (best == 0 || cost < best) best = cost, pick = p;
         }
         if (best != 0) break;
@@ -716,7 +777,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
         cfg.numAttrs = 1;
     }
     void *args[1] = {&pick};
-    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel((pick.cols + 7) / 8, gb), args);
+    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb), args);
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     count_launch();
     return SQ_OK;
