@@ -258,6 +258,7 @@ constexpr int kUnitBytes = kTileN * kUnitK / 2;
 constexpr int kMaxStages = 4;        // of a warp's ring; 2 or 3 where the activations leave no room for more
 constexpr int kRedPitch = 20;        // floats per column of a tile's sums (16 used; 20 keeps the stores off one bank)
 constexpr int kMaxCols = 48;         // columns of a pass: 16 rows of three bytes each
+constexpr int kAhead = 3;            // loads of eight activations that a thread has in flight
 constexpr int kMaxBlock = 128;       // inputs that share a fixed-point range: a group, or this many of a longer one
 
 struct MatvecParams {
@@ -393,6 +394,38 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
     const uint32_t x_pair = prm.cols * 64;               // 64 codes of all columns
     const uint32_t s_step = prm.unit_groups == GB ? 16 * prm.s_bytes : 0, z_step = prm.unit_groups == GB ? 16 : 0;
 
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
+
+    // raw activations: what a thread converts, kAhead times eight inputs in flight
+    const int eights = U * (kUnitK / 8), all_eights = eights * rows;
+    uint4 raw[kAhead][2];
+    auto is_wide = [&](int i, int &m, int &e, int &k) {
+        m = rows == 1 ? 0 : i / eights;
+        e = i - m * eights;
+        k = u_first * kUnitK + e * 8;
+        return prm.x_wide && k + 8 <= prm.K;
+    };
+    auto fetch = [&](int i) {
+#pragma unroll
+        for (int b = 0; b < kAhead; b++) {
+            int m, e, k;
+            if (i + b * kWarps * 32 < all_eights && is_wide(i + b * kWarps * 32, m, e, k)) {
+                const int64_t at = (m0 + m) * prm.ldx + k;
+                const uint4 *p = prm.x_f32 ? reinterpret_cast<const uint4 *>(static_cast<const float *>(prm.X) + at)
+                                           : reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.X) + at);
+                raw[b][0] = __ldg(p);
+                if (prm.x_f32) raw[b][1] = __ldg(p + 1);
+            }
+        }
+    };
+    fetch(tid);
+    // the bias of this thread's first output
+    float bias0 = 0.0f;
+    if (prm.bias) {
+        const int n = (t_first + (rows == 1 ? (tid * cl + rank) >> 4 : ((tid * cl + rank) >> 4) / rows)) * kTileN + ((tid * cl + rank) & 15);
+        if (n < prm.N) bias0 = __ldg(prm.bias + n);
+    }
+
     for (int t0 = t_first; t0 < t_last; t0 += prm.tiles_round) {
         const int nt_round = min(prm.tiles_round, t_last - t0);
         // this warp's run of the list
@@ -455,12 +488,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         // half of the 64; zero behind the last input, so that whatever lies there in a row of codes counts for nothing.  Whole warps go
         // through the loop: the lanes of a block settle on its range by shuffles.
         if (t0 == t_first) {
-            const int eights = U * (kUnitK / 8), lanes = prm.block / 8;
-            for (int i = tid; i < eights * rows; i += kWarps * 32) {                    // (a multiple of 32)
-                const int m = rows == 1 ? 0 : i / eights, e = i - m * eights, k = u_first * kUnitK + e * 8;
+            const int lanes = prm.block / 8;
+#pragma unroll 1
+            for (int i = tid, b = 0; i < all_eights; i += kWarps * 32) {                // (a multiple of 32)
+                int m, e, k;
                 float x[8];
-                if (prm.x_f32) load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
-                else load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, prm.x_wide);
+                if (is_wide(i, m, e, k)) {
+                    const uint32_t w[8] = {raw[0][0].x, raw[0][0].y, raw[0][0].z, raw[0][0].w, raw[0][1].x, raw[0][1].y, raw[0][1].z, raw[0][1].w};
+#pragma unroll
+                    for (int j = 0; j < 8; j++)
+                        x[j] = prm.x_f32 ? __uint_as_float(w[j]) : __uint_as_float((j & 1) ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+                } else if (prm.x_f32) {
+                    load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, false);
+                } else {
+                    load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, false);
+                }
+#pragma unroll
+                for (int j = 0; j + 1 < kAhead; j++) raw[j][0] = raw[j + 1][0], raw[j][1] = raw[j + 1][1];
+                if (++b == kAhead) b = 0, fetch(i + kWarps * 32);
                 if (prm.act != SQ_ACT_NONE) {
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) unpack2(prm.act == SQ_ACT_SILU ? silu2(x[j], x[j + 1]) : gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
@@ -477,12 +522,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 for (int j = 0; j < 8; j++)
                     v[j] = (__float_as_uint(finite ? fmaf(x[j], up, kRoundMagic) : kRoundMagic) - (0x4B400000u - 0x808080u)) ^ 0x808080u;
                 uint8_t *dst = smem + prm.x_off + size_t(e >> 3) * x_pair + (e & 3) * 16 + (e >> 2 & 1) * 8;
-                int sum[3];
+                int sum[3] = {0, 0, 0};
 #pragma unroll
                 for (int p = 0; p < 3; p++) {
                     const uint2 b = make_uint2(bytes_of(v[0], v[2], v[4], v[6], p), bytes_of(v[1], v[3], v[5], v[7], p));
                     *reinterpret_cast<uint2 *>(dst + (p * prm.rows + m) * 64) = b;
-                    sum[p] = __dp4a(int(b.x), 0x01010101, __dp4a(int(b.y), 0x01010101, 0));
+                    if (prm.z) sum[p] = __dp4a(int(b.x), 0x01010101, __dp4a(int(b.y), 0x01010101, 0));
                 }
                 if (prm.z) {
                     for (int d = 1; d < lanes; d <<= 1) {
@@ -491,7 +536,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                     }
                 }
                 if (lane % lanes == 0) {
-                    const int at = (i - m * eights) / lanes * prm.cols8 + m;
+                    const int at = e / lanes * prm.cols8 + m;
                     float *f = reinterpret_cast<float *>(smem + prm.f_off) + at;
                     int *xs = reinterpret_cast<int *>(smem + prm.xs_off) + at;
 #pragma unroll
@@ -600,7 +645,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
             const int c = o & 15, q = o >> 4, tl = rows == 1 ? q : q / rows, m = q - tl * rows, n = (t0 + tl) * kTileN + c;
             if (n >= prm.N) continue;
-            float v = prm.bias ? __ldg(prm.bias + n) : 0.0f;
+            float v = bias0;
+            if (prm.bias && (t0 != t_first || o >= kWarps * 32 * cl)) v = __ldg(prm.bias + n);
             for (int r = 0; r < cl; r++) {
                 const int Ur = min(prm.units - r * prm.units_cta, prm.units_cta), sum_units = nt_round * Ur;
                 if (Ur <= 0) break;
@@ -768,14 +814,14 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = smem_bytes(pick);
     cfg.stream = st;
-    cudaLaunchAttribute at{};
-    if (pick.cl > 1) {
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim.x = unsigned(pick.cl);
-        at.val.clusterDim.y = at.val.clusterDim.z = 1;
-        cfg.attrs = &at;
-        cfg.numAttrs = 1;
-    }
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = unsigned(pick.cl);
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pick.cl > 1 ? 2 : 1;
     void *args[1] = {&pick};
     const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb), args);
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
