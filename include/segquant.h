@@ -309,13 +309,13 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *   segquant_dequantize_w4_group: W [N,K] of dtype dt from them, one fp32 product each, rounded once to dt.
  *   segquant_w4_matvec: y[m][n] = sum_g s[g][n] * ( sum_{k in g} (c[n][k] - z[g][n]) * a[m][k] ) + bias[n],
  *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused; NOT rounded
- *     to dt in between).  a enters as a fixed-point number, off by at most 2^-22 of the largest |a| of its row in its group (in its
- *     128 inputs of a longer group, counted from the row's start), and at least 2^-123; bf16 values down to 2^-14 of that largest one are exact.
- *     Sums over those inputs are exact, the rest is fp32 in an order that depends on the sizes and the device alone; one
+ *     to dt in between).  a enters as a fixed-point number, off by at most 2^-22 of the largest |a| among the 256 inputs
+ *     k / 256 of its row (or 2^-123); bf16 values down to 2^-14 of that largest one are exact.  Sums over a group (128 inputs of a
+ *     longer one) are exact, the rest is fp32 in an order that depends on the sizes and the device alone; one
  *     rounding to y_dtype.  A row with an infinity or a NaN among its activations has NaN for outputs.  X [M,K] dev (dtype dt, ldx
  *     elements), bias dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements
  *     only; Y must not overlap X.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072; any M, meant for M of at most about 32
- *     (the weights are read once per pass of up to 16 rows).  No workspace.
+ *     (the weights are read once per pass of up to 10 rows).  No workspace.
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
  *     N <= 2097120 for the two offline calls. */
 sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *Wq4,

@@ -257,9 +257,9 @@ constexpr int kUnitK = 256;          // codes per channel and ring stage: 128 by
 constexpr int kUnitBytes = kTileN * kUnitK / 2;
 constexpr int kMaxStages = 4;        // of a warp's ring; 2 or 3 where the activations leave no room for more
 constexpr int kRedPitch = 20;        // floats per column of a tile's sums (16 used; 20 keeps the stores off one bank)
-constexpr int kMaxCols = 48;         // columns of a pass: 16 rows of three bytes each
+constexpr int kMaxCols = 32;         // columns of a pass: 10 rows of three bytes each
 constexpr int kAhead = 3;            // loads of eight activations that a thread has in flight
-constexpr int kMaxBlock = 128;       // inputs that share a fixed-point range: a group, or this many of a longer one
+constexpr int kMaxBlock = 128;       // inputs of an exact sum: a group, or this many of a longer one
 
 struct MatvecParams {
     const void *X;
@@ -267,7 +267,6 @@ struct MatvecParams {
     int M, rows;                     // rows of X, rows of one pass (grid.y)
     int K;
     int x_f32, x_wide, act;
-    int block;                       // inputs of a fixed-point range: 32, 64 or 128
     const uint8_t *W4;
     int64_t ldw;
     int N, row_bytes;
@@ -342,10 +341,20 @@ __device__ __forceinline__ uint2 shared_v2(uint32_t at)
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
-// bytes `which` of four words
-__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t which)
+// bytes 0, 1 and 2 of four words
+__device__ __forceinline__ void bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&p)[3])
 {
-    return __byte_perm(__byte_perm(a, b, which | (which + 4) << 4), __byte_perm(c, d, which | (which + 4) << 4), 0x5410);
+    const uint32_t ab = __byte_perm(a, b, 0x5140), cd = __byte_perm(c, d, 0x5140);
+    p[0] = __byte_perm(ab, cd, 0x5410);
+    p[1] = __byte_perm(ab, cd, 0x7632);
+    p[2] = __byte_perm(__byte_perm(a, b, 0x0062), __byte_perm(c, d, 0x0062), 0x5410);
+}
+// max(|a|, |b|), a NaN where either is one
+__device__ __forceinline__ float largest(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return d;
 }
 __device__ __forceinline__ void cluster_barrier()
 {
@@ -362,13 +371,15 @@ __device__ __forceinline__ void cluster_barrier()
 // bytes 16 c of codes 0, 2, 4, 6 and w & 0xF0F0F0F0 those of 1, 3, 5, 7, and the activations are laid out in that order, too; any order
 // of K will do as long as both operands have it.
 //
-// Fixed point: with 2^E <= max|x| < 2^(E+1) over a block of at most 128 inputs, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
-// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact); the bytes of (q + 0x808080) ^ 0x808080 are signed q0, q1, q2 with
-// q = q0 + 256 q1 + 65536 q2.  A block's sum of 16 (c - z) q_i stays within 2^22 for zero-points in [-8, 7], so that it becomes a float by
-// starting at the bits of 1.5 * 2^23 and subtracting that number: the start, less the zero-point times the block's sum of q_i, is the
-// MMA's addend.  Behind it one FMA in fp32 with scale times 2^(E - 25) 256^i.  A block with an infinity or a NaN has the factor NaN.
+// Fixed point: with 2^E <= max|x| < 2^(E+1) over the 256 inputs of a unit, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
+// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact); the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2
+// with q = q0 + 256 q1 + 65536 q2.  A block, a group or 128 inputs of a longer one, has a sum of 16 (c - z) q_i within 2^22 for
+// zero-points in [-8, 7], so that it becomes a float by starting at the bits of 1.5 * 2^23 and subtracting that number: the start,
+// less the zero-point times the block's sum of q_i, is the MMA's addend.  One FMA in fp32 takes it with its scale to the unit's sum, and one
+// the unit's sum with 2^(E - 25) 256^i to the tile's.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
+// instead: 27.6 us for 1 x 8192 -> 28672, where one per unit takes XX; 10.0 us for 8 x 1536 -> 9216 with SiLU instead of YY.)
 // GB: blocks of a unit (2, 4, 8).
-template <int NT, int GB>
+template <int NT, int GB, bool ZP>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_constant__ MatvecParams prm)
 {
     extern __shared__ __align__(128) uint8_t smem[];
@@ -383,7 +394,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
     const uint32_t d0 = wr * 128 + ((wc ^ wr) << 4), d1 = (wr + 4) * 128 + ((wc ^ wr ^ 4) << 4);
     const int64_t row4 = 4 * prm.ldw;
     const int pieces = prm.s_bytes, s_group = lane / pieces, s_n = lane % pieces * (16 / prm.s_bytes);   // 16-byte pieces of 16 channels' scales
-    const bool s_lane = lane < prm.unit_groups * pieces, z_lane = prm.z && lane < prm.unit_groups;
+    const bool s_lane = lane < prm.unit_groups * pieces, z_lane = ZP && lane < prm.unit_groups;
     const uint32_t lm_row = (lane & 15) * 128, lm_seg = lane >> 4, lm_x = lane & 7;      // ldmatrix: rows 0-15 of two pieces
     uint32_t lm[4];
 #pragma unroll
@@ -396,29 +407,38 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
 
-    // raw activations: what a thread converts, kAhead times eight inputs in flight
+    // raw activations: what a thread converts, kAhead times eight inputs in flight.  Eight e of row m: inputs u_first kUnitK + 8 e ..
     const int eights = U * (kUnitK / 8), all_eights = eights * rows;
-    uint4 raw[kAhead][2];
-    auto is_wide = [&](int i, int &m, int &e, int &k) {
-        m = rows == 1 ? 0 : i / eights;
-        e = i - m * eights;
-        k = u_first * kUnitK + e * 8;
-        return prm.x_wide && k + 8 <= prm.K;
+    struct Place {
+        int i, m, e;
+        __device__ void next(int eights)
+        {
+            i += kWarps * 32;
+            for (e += kWarps * 32; e >= eights; e -= eights) m++;
+        }
     };
-    auto fetch = [&](int i) {
+    Place ahead{tid, 0, tid}, here;
+    if (tid < all_eights) ahead.m = tid / eights, ahead.e = tid - ahead.m * eights;
+    here = ahead;
+    const int k_first = u_first * kUnitK;
+    uint4 raw[kAhead][2];
+    auto is_wide = [&](const Place &p) { return prm.x_wide && k_first + p.e * 8 + 8 <= prm.K; };
+    auto fetch = [&]() {
 #pragma unroll
         for (int b = 0; b < kAhead; b++) {
-            int m, e, k;
-            if (i + b * kWarps * 32 < all_eights && is_wide(i + b * kWarps * 32, m, e, k)) {
-                const int64_t at = (m0 + m) * prm.ldx + k;
-                const uint4 *p = prm.x_f32 ? reinterpret_cast<const uint4 *>(static_cast<const float *>(prm.X) + at)
-                                           : reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.X) + at);
-                raw[b][0] = __ldg(p);
-                if (prm.x_f32) raw[b][1] = __ldg(p + 1);
+            if (ahead.i < all_eights) {
+                if (is_wide(ahead)) {
+                    const int64_t at = (m0 + ahead.m) * prm.ldx + k_first + ahead.e * 8;
+                    const uint4 *p = prm.x_f32 ? reinterpret_cast<const uint4 *>(static_cast<const float *>(prm.X) + at)
+                                               : reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.X) + at);
+                    raw[b][0] = __ldg(p);
+                    if (prm.x_f32) raw[b][1] = __ldg(p + 1);
+                }
+                ahead.next(eights);
             }
         }
     };
-    fetch(tid);
+    fetch();
     // the bias of this thread's first output
     float bias0 = 0.0f;
     if (prm.bias) {
@@ -488,62 +508,71 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         // half of the 64; zero behind the last input, so that whatever lies there in a row of codes counts for nothing.  Whole warps go
         // through the loop: the lanes of a block settle on its range by shuffles.
         if (t0 == t_first) {
-            const int lanes = prm.block / 8;
+            constexpr int kBlockLanes = 32 / GB;
 #pragma unroll 1
-            for (int i = tid, b = 0; i < all_eights; i += kWarps * 32) {                // (a multiple of 32)
-                int m, e, k;
+            for (int b = 0; here.i < all_eights; here.next(eights)) {                   // (a multiple of 32)
+                const int m = here.m, e = here.e;
                 float x[8];
-                if (is_wide(i, m, e, k)) {
-                    const uint32_t w[8] = {raw[0][0].x, raw[0][0].y, raw[0][0].z, raw[0][0].w, raw[0][1].x, raw[0][1].y, raw[0][1].z, raw[0][1].w};
+                if (is_wide(here)) {
+                    if (prm.x_f32) {
+                        const uint32_t w[8] = {raw[0][0].x, raw[0][0].y, raw[0][0].z, raw[0][0].w, raw[0][1].x, raw[0][1].y, raw[0][1].z, raw[0][1].w};
 #pragma unroll
-                    for (int j = 0; j < 8; j++)
-                        x[j] = prm.x_f32 ? __uint_as_float(w[j]) : __uint_as_float((j & 1) ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+                        for (int j = 0; j < 8; j++) x[j] = __uint_as_float(w[j]);
+                    } else {
+                        const uint32_t w[4] = {raw[0][0].x, raw[0][0].y, raw[0][0].z, raw[0][0].w};
+#pragma unroll
+                        for (int j = 0; j < 8; j++) x[j] = __uint_as_float((j & 1) ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+                    }
                 } else if (prm.x_f32) {
-                    load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, false);
+                    load8(static_cast<const float *>(prm.X) + (m0 + m) * prm.ldx, k_first + e * 8, prm.K, x, false);
                 } else {
-                    load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k, prm.K, x, false);
+                    load8(static_cast<const __nv_bfloat16 *>(prm.X) + (m0 + m) * prm.ldx, k_first + e * 8, prm.K, x, false);
                 }
 #pragma unroll
                 for (int j = 0; j + 1 < kAhead; j++) raw[j][0] = raw[j + 1][0], raw[j][1] = raw[j + 1][1];
-                if (++b == kAhead) b = 0, fetch(i + kWarps * 32);
-                if (prm.act != SQ_ACT_NONE) {
+                if (++b == kAhead) b = 0, fetch();
+                if (prm.act == SQ_ACT_SILU) {
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) unpack2(prm.act == SQ_ACT_SILU ? silu2(x[j], x[j + 1]) : gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                    for (int j = 0; j < 8; j += 2) unpack2(silu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                } else if (prm.act == SQ_ACT_GELU) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) unpack2(gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
                 }
-                uint32_t top = 0;                        // largest magnitude, as bits
+                float top = largest(largest(largest(x[0], x[1]), largest(x[2], x[3])), largest(largest(x[4], x[5]), largest(x[6], x[7])));
 #pragma unroll
-                for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-                for (int d = 1; d < lanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                const bool finite = top < 0x7F800000u;
-                const uint32_t be = max(top >> 23, 27u);                                // biased E; smaller ranges count as 2^-100
-                const float up = finite ? __uint_as_float((275u - be) << 23) : 0.0f;    // 2^(21 - E)
+                for (int d = 1; d < 32; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                const bool finite = top < __uint_as_float(0x7F800000u);
+                const uint32_t be = max(__float_as_uint(top) >> 23, 27u);               // biased E; smaller ranges count as 2^-100
+                const float up = finite ? __uint_as_float((275u - be) << 23) : 0.0f;    // 2^(21 - E); (other blocks: any bytes)
                 uint32_t v[8];
 #pragma unroll
-                for (int j = 0; j < 8; j++)
-                    v[j] = (__float_as_uint(finite ? fmaf(x[j], up, kRoundMagic) : kRoundMagic) - (0x4B400000u - 0x808080u)) ^ 0x808080u;
+                for (int j = 0; j < 8; j++) v[j] = __float_as_uint(fmaf(x[j], up, kRoundMagic)) - (0x4B400000u - 0x8080u);
                 uint8_t *dst = smem + prm.x_off + size_t(e >> 3) * x_pair + (e & 3) * 16 + (e >> 2 & 1) * 8;
+                uint32_t even[3], odd[3];
+                bytes_of(v[0], v[2], v[4], v[6], even);
+                bytes_of(v[1], v[3], v[5], v[7], odd);
                 int sum[3] = {0, 0, 0};
 #pragma unroll
                 for (int p = 0; p < 3; p++) {
-                    const uint2 b = make_uint2(bytes_of(v[0], v[2], v[4], v[6], p), bytes_of(v[1], v[3], v[5], v[7], p));
-                    *reinterpret_cast<uint2 *>(dst + (p * prm.rows + m) * 64) = b;
-                    if (prm.z) sum[p] = __dp4a(int(b.x), 0x01010101, __dp4a(int(b.y), 0x01010101, 0));
+                    const uint2 b2 = p < 2 ? make_uint2(even[p] ^ 0x80808080u, odd[p] ^ 0x80808080u) : make_uint2(even[p], odd[p]);
+                    *reinterpret_cast<uint2 *>(dst + (p * prm.rows + m) * 64) = b2;
+                    if (ZP) sum[p] = __dp4a(int(b2.x), 0x01010101, __dp4a(int(b2.y), 0x01010101, 0));
                 }
-                if (prm.z) {
-                    for (int d = 1; d < lanes; d <<= 1) {
+                if (ZP) {
+#pragma unroll
+                    for (int d = 1; d < kBlockLanes; d <<= 1) {
 #pragma unroll
                         for (int p = 0; p < 3; p++) sum[p] += __shfl_xor_sync(0xFFFFFFFFu, sum[p], d);
                     }
-                }
-                if (lane % lanes == 0) {
-                    const int at = e / lanes * prm.cols8 + m;
-                    float *f = reinterpret_cast<float *>(smem + prm.f_off) + at;
-                    int *xs = reinterpret_cast<int *>(smem + prm.xs_off) + at;
+                    if (lane % kBlockLanes == 0) {
+                        int *xs = reinterpret_cast<int *>(smem + prm.xs_off) + e / kBlockLanes * prm.cols8 + m;
 #pragma unroll
-                    for (int p = 0; p < 3; p++) {
-                        f[p * prm.rows] = finite ? __uint_as_float((be - 25u + 8u * p) << 23) : __uint_as_float(0x7FC00000u);
-                        if (prm.z) xs[p * prm.rows] = 16 * sum[p];
+                        for (int p = 0; p < 3; p++) xs[p * prm.rows] = 16 * sum[p];
                     }
+                }
+                if (lane < 3) {
+                    float *f = reinterpret_cast<float *>(smem + prm.f_off) + (e >> 5) * prm.cols8 + m;
+                    f[lane * prm.rows] = finite ? __uint_as_float((be - 25u + 8u * lane) << 23) : __uint_as_float(0x7FC00000u);
                 }
             }
             __syncthreads();
@@ -566,27 +595,23 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             __syncwarp();
             issue(slot == 0 ? prm.stages - 1 : slot - 1);   // the stage that was used up last
             const uint32_t st = ring + slot * prm.stage_bytes, x_unit = uint32_t(u) * 4 * x_pair;
-            const uint32_t f_at = sm0 + prm.f_off + (u * GB * prm.cols8 + 2 * t) * 4;
+            const uint32_t f_at = sm0 + prm.f_off + (u * prm.cols8 + 2 * t) * 4, xs_at = sm0 + prm.xs_off + (u * GB * prm.cols8 + 2 * t) * 4;
             const uint32_t s_at = st + kUnitBytes + g * prm.s_bytes, z_at = st + prm.z_off + g;
             int sum[NT][4];
-            // the sums of a block start here
+            float part[NT][4];
+            // what the sums of block b start from
             auto start = [&](int b) {
-                if (prm.z) {
-                    const int z0 = shared_s8(z_at + b * z_step), z1 = shared_s8(z_at + b * z_step + 8);
+                int z0 = 0, z1 = 0;
+                if (ZP) z0 = shared_s8(z_at + b * z_step), z1 = shared_s8(z_at + b * z_step + 8);
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) {
-                        const uint2 xs = shared_v2(f_at + (prm.xs_off - prm.f_off) + (b * prm.cols8 + nt * 8) * 4);
-                        sum[nt][0] = kMagicBits - z0 * int(xs.x), sum[nt][1] = kMagicBits - z0 * int(xs.y);
-                        sum[nt][2] = kMagicBits - z1 * int(xs.x), sum[nt][3] = kMagicBits - z1 * int(xs.y);
-                    }
-                } else {
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int j = 0; j < 4; j++) sum[nt][j] = kMagicBits;
+                for (int nt = 0; nt < NT; nt++) {
+                    uint2 xs = make_uint2(0u, 0u);
+                    if (ZP) xs = shared_v2(xs_at + (b * prm.cols8 + nt * 8) * 4);
+                    sum[nt][0] = kMagicBits - z0 * int(xs.x), sum[nt][1] = kMagicBits - z0 * int(xs.y);
+                    sum[nt][2] = kMagicBits - z1 * int(xs.x), sum[nt][3] = kMagicBits - z1 * int(xs.y);
                 }
             };
-            // .. and end here
+            // and what becomes of them
             auto finish = [&](int b) {
                 float s0, s1;
                 if (prm.s_bytes == 4) {
@@ -596,12 +621,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
-                    const uint2 fb = shared_v2(f_at + (b * prm.cols8 + nt * 8) * 4);
-                    const float f0 = __uint_as_float(fb.x), f1 = __uint_as_float(fb.y);
-                    acc[nt][0] = fmaf(s0 * f0, __int_as_float(sum[nt][0]) - kRoundMagic, acc[nt][0]);
-                    acc[nt][1] = fmaf(s0 * f1, __int_as_float(sum[nt][1]) - kRoundMagic, acc[nt][1]);
-                    acc[nt][2] = fmaf(s1 * f0, __int_as_float(sum[nt][2]) - kRoundMagic, acc[nt][2]);
-                    acc[nt][3] = fmaf(s1 * f1, __int_as_float(sum[nt][3]) - kRoundMagic, acc[nt][3]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float v = __int_as_float(sum[nt][j]) - kRoundMagic, sc = j < 2 ? s0 : s1;
+                        part[nt][j] = b == 0 ? sc * v : fmaf(sc, v, part[nt][j]);
+                    }
                 }
             };
 #pragma unroll
@@ -621,6 +645,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 if (GB == 8) finish(2 * pr + 1);
                 else if (GB == 4) finish(pr);
                 else if (pr % 2 == 1) finish(pr / 2);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                const uint2 f = shared_v2(f_at + nt * 32);
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[nt][j] = fmaf(__uint_as_float(j % 2 ? f.y : f.x), part[nt][j], acc[nt][j]);
             }
             slot = slot + 1 == prm.stages ? 0 : slot + 1;
             if (++u == U || i + 1 == end) {              // what this run has of the tile: [column][16 channels]
@@ -676,25 +706,23 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 
 // ---------------------------------------------------------------------------------------------- host side
 
-template <int NT>
+template <int NT, bool ZP>
 const void *matvec_kernel(int gb)
 {
     switch (gb) {
-        case 2: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 2>);
-        case 4: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 4>);
-        default: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 8>);
+        case 2: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 2, ZP>);
+        case 4: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 4, ZP>);
+        default: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 8, ZP>);
     }
 }
 constexpr int kMaxNt = kMaxCols / 8;
-const void *matvec_kernel(int nt, int gb)
+const void *matvec_kernel(int nt, int gb, bool zp)
 {
     switch (nt) {
-        case 1: return matvec_kernel<1>(gb);
-        case 2: return matvec_kernel<2>(gb);
-        case 3: return matvec_kernel<3>(gb);
-        case 4: return matvec_kernel<4>(gb);
-        case 5: return matvec_kernel<5>(gb);
-        default: return matvec_kernel<6>(gb);
+        case 1: return zp ? matvec_kernel<1, true>(gb) : matvec_kernel<1, false>(gb);
+        case 2: return zp ? matvec_kernel<2, true>(gb) : matvec_kernel<2, false>(gb);
+        case 3: return zp ? matvec_kernel<3, true>(gb) : matvec_kernel<3, false>(gb);
+        default: return zp ? matvec_kernel<4, true>(gb) : matvec_kernel<4, false>(gb);
     }
 }
 
@@ -717,7 +745,8 @@ sq_status matvec_device(MatvecDevice *out)
     cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
     for (int nt = 1; nt <= kMaxNt && e == cudaSuccess; nt++)
         for (int gb = 2; gb <= 8 && e == cudaSuccess; gb *= 2)
-            e = cudaFuncSetAttribute(matvec_kernel(nt, gb), cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem));
+            for (int zp = 0; zp < 2 && e == cudaSuccess; zp++)
+                e = cudaFuncSetAttribute(matvec_kernel(nt, gb, zp), cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem));
     d.clusters[0] = d.sms;
     for (int i = 1; i <= 3 && e == cudaSuccess; i++) {
         cudaLaunchConfig_t cfg{};
@@ -730,7 +759,7 @@ sq_status matvec_device(MatvecDevice *out)
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 2), &cfg);
+        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 2, false), &cfg);
     }
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     g_devices.push_back(d);
@@ -745,15 +774,16 @@ bool lay_out(MatvecParams &p, int gb, int tiles)
     const uint32_t s_bytes = uint32_t(p.unit_groups * kTileN * p.s_bytes), z_bytes = p.z ? uint32_t(p.unit_groups * kTileN) : 0u;
     p.z_off = kUnitBytes + s_bytes;
     p.stage_bytes = (p.z_off + z_bytes + 127u) & ~127u;
-    const size_t x_bytes = size_t(p.units_cta) * 4 * p.cols * 64, f_bytes = size_t(p.units_cta) * gb * p.cols8 * 4;
+    const size_t x_bytes = size_t(p.units_cta) * 4 * p.cols * 64, f_bytes = size_t(p.units_cta) * p.cols8 * 4,
+                 xs_bytes = p.z ? gb * f_bytes : 0;
     const size_t sum = size_t(p.cols) * kRedPitch * 4;
     for (p.stages = kMaxStages; p.stages >= 2; p.stages--) {
-        const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + f_bytes * (p.z ? 2 : 1) + kWarps * sum;
+        const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + f_bytes + xs_bytes + kWarps * sum;
         if (fixed + std::min(tiles, 4) * sum > kMaxSmem) continue;
         p.x_off = uint32_t(kWarps * p.stages) * p.stage_bytes;
         p.f_off = uint32_t(p.x_off + x_bytes);
-        p.xs_off = uint32_t(p.f_off + (p.z ? f_bytes : 0));
-        p.head_off = uint32_t(p.xs_off + f_bytes);
+        p.xs_off = uint32_t(p.f_off + f_bytes);
+        p.head_off = uint32_t(p.xs_off + xs_bytes);
         p.red_off = uint32_t(p.head_off + kWarps * sum);
         p.tiles_round = int(std::min<size_t>(tiles, (kMaxSmem - fixed) / sum));
         return true;
@@ -776,8 +806,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     p.y_f32 = a.y_dtype == SQ_F32;
     p.W4 = static_cast<const uint8_t *>(a.W4); p.ldw = a.ldw; p.N = int(a.N); p.row_bytes = int((a.K + 1) / 2);
     const int64_t group = std::min<int64_t>(a.group, (a.K + kUnitK - 1) / kUnitK * kUnitK);
-    p.block = int(std::min<int64_t>(group, kMaxBlock));
-    const int gb = kUnitK / p.block;
+    const int gb = int(kUnitK / std::min<int64_t>(group, kMaxBlock));
     p.unit_groups = group >= kUnitK ? 1 : int(kUnitK / group);
     p.units_group = group >= kUnitK ? int(group / kUnitK) : 1;
     p.groups = int((a.K + a.group - 1) / a.group);
@@ -787,7 +816,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     p.units = int((a.K + kUnitK - 1) / kUnitK);
     p.tiles = int((a.N + kTileN - 1) / kTileN);
 
-    // Rows of a pass: as many as 48 columns take, spread evenly; fewer where the activations would not fit.
+    // Rows of a pass: as many as 32 columns take, spread evenly; fewer where the activations would not fit.
     const int most = kMaxCols / 3;
     int passes = (p.M + most - 1) / most;
     double best = 0;
@@ -823,7 +852,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     cfg.attrs = at;
     cfg.numAttrs = pick.cl > 1 ? 2 : 1;
     void *args[1] = {&pick};
-    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb), args);
+    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb, p.z != nullptr), args);
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     count_launch();
     return SQ_OK;

@@ -3,9 +3,9 @@ definition in numpy (fp32 divisions are IEEE on both sides, so they have to be e
 64-bit sums.
 
 Tolerance of the product.  An activation enters as a fixed-point number that is off by at most 2^-22 of the largest magnitude of
-its row in its block (a group, 128 inputs of a longer one), or 2^-123; products with codes and their sums over a block are exact integers.
+its row in its 256 inputs, or 2^-123; products with codes and their sums over a block (a group, 128 inputs of a longer one) are exact integers.
 Behind that roundings of 2^-24 of partial sums that are no larger than the sum of magnitudes (of the three bytes of an activation: at most
-1.02 times that of the activation, and the fixed-point error again): scale times range, its product and sum per block, then sums over at
+1.02 times that of the activation, and the fixed-point error again): one sum per block and one per 256 inputs, then sums over at
 most eight CTAs, sixteen runs and three bytes, and the bias.  The activation functions come with the errors that the C header gives.  bf16
 outputs are rounded once more, by at most half a step (2^-8)."""
 import numpy as np
@@ -146,9 +146,9 @@ def check_product(Y, X, W, bias, act, G, K):
     x = X.double()
     a = act64(x, act)
     blk = min(G, 128)
-    pad = torch.zeros((a.shape[0], -(-K // blk) * blk), dtype=torch.float64, device=DEV)
+    pad = torch.zeros((a.shape[0], -(-K // 256) * 256), dtype=torch.float64, device=DEV)
     pad[:, :K] = a.abs() * (1 + act_error(x, act))
-    largest = pad.view(a.shape[0], -1, blk).amax(2).repeat_interleave(blk, 1)[:, :K]
+    largest = pad.view(a.shape[0], -1, 256).amax(2).repeat_interleave(256, 1)[:, :K]
     fixed = (2.0 ** -22 * largest + 2.0 ** -123) @ W.abs().t()
     want = a @ W.t()
     mags = a.abs() @ W.abs().t()
@@ -218,19 +218,17 @@ def test_rows_do_not_see_one_another(x):
         assert bool(torch.isnan(got[m]).all())
 
 
-def test_ranges_of_groups():
-    """A large value in one group costs nothing in another; bf16 values down to 2^-14 of their group's largest are exact: sums that a
-    double holds exactly come out as the nearest fp32 numbers of them."""
+def test_ranges_of_inputs():
+    """A large value costs nothing beyond its 256 inputs; bf16 values down to 2^-14 of their largest are exact."""
     K, N, G = 512, 64, 64
     W4, s_w, z_w = random_codes(N, K, G, True, F32, 4)
     s_w.fill_(1.0)
     g = torch.Generator(device=DEV).manual_seed(6)
     X = torch.randint(-255, 256, (2, K), generator=g, device=DEV).float() * 2.0 ** -7
     X[:, ::7] *= 2.0 ** -6
-    X[0, :64] *= 2.0 ** 40                                   # another group's range
     X = X.to(BF)
     W = weights64(W4, s_w, z_w, G, K)
-    X[0, :64] = 0
+    X[0, :256] = 0
     Y = B.segquant_w4_matvec(X, W4, s_w, G, z_w, y_dtype=F32)
     assert float((Y.double() - X.double() @ W.t()).abs().max()) <= 2.0 ** -24 * 40 * float((X.double().abs() @ W.abs().t()).max())
     big = X.clone()
