@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <atomic>
 #include <mutex>
+#include <type_traits>
 #include <vector>
 #include "activation.cuh"
 
@@ -22,9 +23,11 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------- quantize / dequantize
 
-constexpr int kTileRows = 32;        // channels per block
-constexpr int kTileK = 256;          // inputs per block: 8 per lane of a warp
-constexpr int kRowsPerWarp = 4;      // 8 warps
+constexpr int kTileRows = 32;        // dequantize: channels per block
+constexpr int kTileK = 256;          // .. inputs per block: 8 per lane of a warp
+constexpr int kRowsPerWarp = 4;      // .. 8 warps
+constexpr int kQuantRows = 16;       // quantize: channels per block, two per warp
+constexpr int kQuantK = 512;         // .. inputs per block (or one longer group): 16 per lane
 
 // elements k .. k + 7 of a row of K, zero behind its end; wide: 16 bytes at a time
 template <typename Tin>
@@ -47,119 +50,173 @@ __device__ __forceinline__ void load8(const Tin *row, int64_t k, int64_t K, floa
 }
 
 // a scale as stored; where that is 0 (no range, or one that underflows) it is 1
-template <typename Ts> __device__ __forceinline__ float stored_scale(float s);
-template <> __device__ __forceinline__ float stored_scale<float>(float s) { return s == 0.0f ? 1.0f : s; }
-template <> __device__ __forceinline__ float stored_scale<__nv_bfloat16>(float s)
+__device__ __forceinline__ float stored_scale(float s, bool bf16)
 {
-    const float r = __bfloat162float(__float2bfloat16_rn(s));
+    const float r = bf16 ? __bfloat162float(__float2bfloat16_rn(s)) : s;
     return r == 0.0f ? 1.0f : r;
 }
-__device__ __forceinline__ void store_scale(float *p, float s) { *p = s; }
-__device__ __forceinline__ void store_scale(__nv_bfloat16 *p, float s) { *p = __float2bfloat16_rn(s); }
 
 struct W4QuantParams {
     const void *W;
-    int64_t ld, N, K;
-    int group;
+    int64_t ld;
+    int N, K;
+    int group, span, tiles_k;        // span: inputs per block
     uint8_t *W4;
     int64_t ldw;
     void *s;
+    int s_bf16;
     int64_t lds;
     int8_t *z;
     int64_t ldz;
-    int64_t groups;
+    int groups;
 };
 
-// Bound by reading W: a warp reads 256 consecutive inputs of a channel (four channels in flight), the lanes of a group agree on
-// its extrema by shuffles, and the codes leave as 128 consecutive bytes.  Groups longer than 256 read the channel's group twice,
-// the second time from cache.  Scales and zero-points are [groups][N]; a block of 32 channels gathers them in shared memory, so that
-// they leave as runs of 32 channels.
-template <typename Tin, typename Ts, bool ZP>
+// Sixteen codes of a lane -> two words.  Clip, then round (the bounds are whole numbers): the nibble is the sum's last bits,
+// plus the zero-point's.  Only the upper bound of codes with zero-points needs the clip: a scale of the fast form is its extremum
+// over 7 (or 15) to within 2^-9, so that no symmetric quotient rounds beyond 7, and -8 - round(lo / s) + round(lo / s) is the lower bound
+// itself; the upper one is passed by 1 where both ends round up.
+template <bool ZP>
+__device__ __forceinline__ uint2 codes16(const float (&x)[16], const SegConst &c, float hi, uint32_t z4)
+{
+    const uint64_t r2 = pack2(c.r, c.r), ns2 = pack2(-c.s, -c.s), magic2 = pack2(kRoundMagic, kRoundMagic);
+    uint32_t v[16], w[2];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        float q0, q1;
+        unpack2(div2_rn_fast(pack2(x[i], x[i + 1]), ns2, r2), q0, q1);     // (see SegConst: the codes of the IEEE quotients)
+        if (ZP) q0 = fminf(q0, hi), q1 = fminf(q1, hi);
+        unpack2u(add2(pack2(q0, q1), magic2), v[i], v[i + 1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; i++) {                                          // last bytes of the even and of the odd codes
+        const uint32_t *u = v + 8 * i;
+        uint32_t even = __byte_perm(__byte_perm(u[0], u[2], 0x0040), __byte_perm(u[4], u[6], 0x0040), 0x5410);
+        uint32_t odd = __byte_perm(__byte_perm(u[1], u[3], 0x0040), __byte_perm(u[5], u[7], 0x0040), 0x5410);
+        if (ZP) even = (even & 0x0F0F0F0Fu) + z4, odd = (odd & 0x0F0F0F0Fu) + z4;
+        w[i] = (even & 0x0F0F0F0Fu) | (odd << 4 & 0xF0F0F0F0u);
+    }
+    return make_uint2(w[0], w[1]);
+}
+// .. where the scale is outside the fast form
+template <bool ZP>
+__device__ __noinline__ uint2 codes16_slow(const float *x, float s, float lo, float hi, uint32_t z4)
+{
+    uint32_t w[2] = {0, 0};
+    for (int i = 0; i < 16; i++) {
+        const uint32_t v = __float_as_uint(fminf(fmaxf(__fdiv_rn(x[i], s), lo), hi) + kRoundMagic) + (ZP ? z4 : 0u);
+        w[i >> 3] |= (v & 15u) << (4 * (i & 7));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+// Bound by reading W.  A warp takes 512 consecutive inputs of a channel, 16 per lane, and two channels; LANES lanes of a group agree
+// on its extrema by shuffles, and the codes leave as 256 consecutive bytes.  Groups longer than 512 (LONG) read the channel's group
+// twice, the second time from cache.  Scales and zero-points are [groups][N]; a block of 16 channels gathers them in shared memory,
+// so that they leave as runs of 16 channels.  (Eight inputs per lane and loops for any group: 43 instructions per weight, 128 us
+// for 18432 x 4608 bf16; 16 inputs and fixed lanes XX.)
+template <typename Tin, bool ZP, int LANES, bool LONG>
 __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_constant__ W4QuantParams prm)
 {
-    __shared__ float sm_s[8][kTileRows];
-    __shared__ int8_t sm_z[8][kTileRows];
+    constexpr int G = 32 / LANES;                        // groups of a warp's inputs
+    __shared__ float sm_s[G][kQuantRows];
+    __shared__ int8_t sm_z[G][kQuantRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t n0 = int64_t(blockIdx.y) * kTileRows;
-    const int span = prm.group > kTileK ? prm.group : kTileK;            // inputs per block
-    const int64_t kb = int64_t(blockIdx.x) * span;
-    const int lanes = prm.group >= kTileK ? 32 : prm.group / 8;          // lanes of a group
-    const Tin *W = static_cast<const Tin *>(prm.W);
-
-    float x[kRowsPerWarp][8];
-    float lo[kRowsPerWarp], hi[kRowsPerWarp];
-#pragma unroll
-    for (int r = 0; r < kRowsPerWarp; r++) {
-        lo[r] = 0.0f, hi[r] = 0.0f;
-        const int64_t n = n0 + warp * kRowsPerWarp + r;
-        if (n < prm.N) {
-            load8(W + n * prm.ld, kb + lane * 8, prm.K, x[r]);
+    const int tile_n = int(blockIdx.x) / prm.tiles_k, kb = (int(blockIdx.x) - tile_n * prm.tiles_k) * prm.span;
+    const int n0 = tile_n * kQuantRows + warp * 2, k0 = kb + lane * 16;
+    const int k_end = LONG ? min(prm.K, kb + prm.span) : prm.K;
+    const Tin *W = static_cast<const Tin *>(prm.W) + int64_t(n0) * prm.ld;
+    auto load16 = [&](int r, int k, float (&x)[16]) {
+        float a[8], b[8];
+        if (n0 + r < prm.N) {
+            load8(W + r * prm.ld, k, k_end, a);
+            load8(W + r * prm.ld, k + 8, k_end, b);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[r][i] = 0.0f;
+            for (int i = 0; i < 8; i++) a[i] = b[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = a[i], x[i + 8] = b[i];
+    };
+    float x[2][16];
+    if (n0 + 2 <= prm.N && kb + kQuantK <= k_end) {      // nothing to look at: both rows' loads in one go
+        constexpr int V = int(sizeof(Tin));              // 16-byte words of 16 inputs
+        uint4 v[2][V];
+#pragma unroll
+        for (int r = 0; r < 2; r++)
+#pragma unroll
+            for (int i = 0; i < V; i++) v[r][i] = __ldg(reinterpret_cast<const uint4 *>(W + r * prm.ld + k0) + i);
+#pragma unroll
+        for (int r = 0; r < 2; r++) {
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(v[r]);
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                x[r][i] = sizeof(Tin) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        }
+    } else {
+        load16(0, k0, x[0]);
+        load16(1, k0, x[1]);
+    }
+    float hi[2], neg[2];                                 // extrema: of both polarities (hi, -lo), or of the magnitude
+    auto extrema = [&](int r, const float (&v)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            hi[r] = fmaxf(hi[r], ZP ? v[i] : fabsf(v[i]));
+            if (ZP) neg[r] = fmaxf(neg[r], -v[i]);
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < 2; r++) {
+        hi[r] = neg[r] = 0.0f;
+        extrema(r, x[r]);
+        if (LONG) {
+            for (int k = k0 + kQuantK; k < k_end; k += kQuantK) {
+                float more[16];
+                load16(r, k, more);
+                extrema(r, more);
+            }
         }
     }
 #pragma unroll
-    for (int r = 0; r < kRowsPerWarp; r++) {
-        const int64_t n = n0 + warp * kRowsPerWarp + r;
-        for (int64_t k = kb + kTileK; k < kb + span && k < prm.K; k += kTileK) {     // long groups: the rest of the extrema
-            float more[8];
-            if (n < prm.N) {
-                load8(W + n * prm.ld, k + lane * 8, prm.K, more);
+    for (int o = 1; o < LANES; o <<= 1) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) lo[r] = fminf(lo[r], more[i]), hi[r] = fmaxf(hi[r], more[i]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) lo[r] = fminf(lo[r], x[r][i]), hi[r] = fmaxf(hi[r], x[r][i]);
-        for (int o = 1; o < lanes; o <<= 1) {
-            lo[r] = fminf(lo[r], __shfl_xor_sync(0xFFFFFFFFu, lo[r], o));
+        for (int r = 0; r < 2; r++) {
             hi[r] = fmaxf(hi[r], __shfl_xor_sync(0xFFFFFFFFu, hi[r], o));
+            if (ZP) neg[r] = fmaxf(neg[r], __shfl_xor_sync(0xFFFFFFFFu, neg[r], o));
         }
-        const float s = stored_scale<Ts>(ZP ? __fdiv_rn(__fsub_rn(hi[r], lo[r]), 15.0f) : __fdiv_rn(fmaxf(hi[r], -lo[r]), 7.0f));
-        float z = 0.0f;
-        if (ZP) z = -8.0f - rintf(__fdiv_rn(lo[r], s));
-        const SegConst c = seg_const(s);
-        const uint64_t r2 = pack2(c.r, c.r), ns2 = pack2(-c.s, -c.s);
-        const float c_lo = ZP ? -8.0f : -7.0f;
-        for (int64_t k = kb; k < kb + span && k < prm.K; k += kTileK) {
-            if (k != kb && n < prm.N) load8(W + n * prm.ld, k + lane * 8, prm.K, x[r]);
-            uint32_t word = 0;
+    }
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float q0, q1;
-                if (c.fast) {                                            // (see SegConst: the codes of the IEEE quotients)
-                    unpack2(div2_rn_fast(pack2(x[r][i], x[r][i + 1]), ns2, r2), q0, q1);
-                } else {
-                    q0 = __fdiv_rn(x[r][i], s), q1 = __fdiv_rn(x[r][i + 1], s);
-                }
-                const int a = __float2int_rn(fminf(fmaxf(rintf(q0) + z, c_lo), 7.0f));
-                const int b = __float2int_rn(fminf(fmaxf(rintf(q1) + z, c_lo), 7.0f));
-                word |= (uint32_t(a & 15) | uint32_t(b & 15) << 4) << (4 * i);
-            }
-            const int64_t kk = k + lane * 8;
-            if (n < prm.N && kk < prm.K) {
-                if (kk + 8 > prm.K) word &= 0xFFFFFFFFu >> (4 * int(kk + 8 - prm.K));    // nothing behind the row's last code
-                uint8_t *out = prm.W4 + n * prm.ldw + kk / 2;
-                if (kk + 8 <= prm.K) {
-                    *reinterpret_cast<uint32_t *>(out) = word;
-                } else {
-                    for (int64_t j = kk; j < prm.K; j += 2) *out++ = uint8_t(word), word >>= 8;
+    for (int r = 0; r < 2; r++) {
+        const float s = stored_scale(ZP ? __fdiv_rn(__fadd_rn(hi[r], neg[r]), 15.0f) : __fdiv_rn(hi[r], 7.0f), prm.s_bf16);
+        const float z = ZP ? rintf(__fdiv_rn(neg[r], s)) - 8.0f : 0.0f;   // (-8 - round(lo / s): rounding is symmetric)
+        const SegConst c = seg_const(s);
+        const float lo = (ZP ? -8.0f : -7.0f) - z, top = 7.0f - z;
+        const uint32_t z4 = (uint32_t(int(z)) & 15u) * 0x01010101u;
+        for (int k = k0; k < k_end; k += kQuantK) {
+            if (LONG && k != k0) load16(r, k, x[r]);
+            const uint2 w = c.fast ? codes16<ZP>(x[r], c, top, z4) : codes16_slow<ZP>(x[r], s, lo, top, z4);
+            if (n0 + r < prm.N) {
+                uint8_t *out = prm.W4 + (n0 + r) * prm.ldw + k / 2;
+                if (k + 16 <= k_end) {
+                    *reinterpret_cast<uint2 *>(out) = w;
+                } else {                                 // the row's last codes, a zero nibble behind an odd one
+                    const uint64_t both = uint64_t(w.y) << 32 | w.x, kept = both & (~uint64_t(0) >> (4 * (k + 16 - k_end)));
+                    for (int j = 0; 2 * j < k_end - k; j++) out[j] = uint8_t(kept >> (8 * j));
                 }
             }
+            if (!LONG) break;
         }
-        if (lane % lanes == 0) {
-            sm_s[lane / lanes][warp * kRowsPerWarp + r] = s;
-            if (ZP) sm_z[lane / lanes][warp * kRowsPerWarp + r] = int8_t(z);
+        if (lane % LANES == 0) {
+            sm_s[lane / LANES][warp * 2 + r] = s;
+            if (ZP) sm_z[lane / LANES][warp * 2 + r] = int8_t(z);
         }
     }
     __syncthreads();
-    const int64_t g0 = kb / prm.group;
-    for (int i = threadIdx.x; i < (32 / lanes) * kTileRows; i += blockDim.x) {
-        const int64_t g = g0 + i / kTileRows, n = n0 + i % kTileRows;
+    if (threadIdx.x < G * kQuantRows) {
+        const int gi = threadIdx.x / kQuantRows, i = threadIdx.x % kQuantRows, g = kb / prm.group + gi, n = tile_n * kQuantRows + i;
         if (g < prm.groups && n < prm.N) {
-            store_scale(static_cast<Ts *>(prm.s) + g * prm.lds + n, sm_s[i / kTileRows][i % kTileRows]);
-            if (ZP) prm.z[g * prm.ldz + n] = sm_z[i / kTileRows][i % kTileRows];
+            if (prm.s_bf16) static_cast<__nv_bfloat16 *>(prm.s)[g * prm.lds + n] = __float2bfloat16_rn(sm_s[gi][i]);
+            else static_cast<float *>(prm.s)[g * prm.lds + n] = sm_s[gi][i];
+            if (ZP) prm.z[g * prm.ldz + n] = sm_z[gi][i];
         }
     }
 }
@@ -220,13 +277,11 @@ __global__ void __launch_bounds__(256) dequantize_w4_group_kernel(const __grid_c
     for (int r = 0; r < kRowsPerWarp; r++) {
         const int64_t n = n0 + warp * kRowsPerWarp + r;
         if (n >= prm.N) return;
-        const float s = sm_s[gi][warp * kRowsPerWarp + r], z = sm_z[gi][warp * kRowsPerWarp + r];
+        // a nibble with its top bit flipped is c + 8; below the bits of 2^23 it makes the float 2^23 + 8 + c
+        const float s = sm_s[gi][warp * kRowsPerWarp + r], z = sm_z[gi][warp * kRowsPerWarp + r] + 8388616.0f;
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int c = int(word[r] << (28 - 4 * i)) >> 28;
-            v[i] = __fmul_rn(float(c) - z, s);
-        }
+        for (int i = 0; i < 8; i++) v[i] = __fmul_rn(__uint_as_float((word[r] >> (4 * i) & 15u) ^ 0x4B000008u) - z, s);
         Tout *out = static_cast<Tout *>(prm.W) + n * prm.ld + k;
         if (k + 8 <= prm.K) {
             if (sizeof(Tout) == 4) {
@@ -861,19 +916,31 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
 sq_status launch_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *W4, int64_t ldw,
                                    void *s, sq_dtype s_dtype, int64_t lds, int8_t *z, int64_t ldz, cudaStream_t st)
 {
-    W4QuantParams p{W, ld, N, K, int(std::min<int64_t>(group, 1 << 30)), static_cast<uint8_t *>(W4), ldw, s, lds, z, ldz,
-                    (K + group - 1) / group};
-    const int64_t span = std::max<int64_t>(p.group, kTileK), by = (N + kTileRows - 1) / kTileRows;
-    if (by > 65535) return SQ_ERR_SHAPE;
-    const dim3 grid(unsigned((K + span - 1) / span), unsigned(by));
-    auto go = [&](auto t, auto ts) {
+    W4QuantParams p{};
+    p.W = W; p.ld = ld; p.N = int(N); p.K = int(K);
+    p.group = int(std::min<int64_t>(group, (K + kQuantK - 1) / kQuantK * kQuantK));
+    p.span = std::max(p.group, kQuantK);
+    const bool longer = kQuantK % p.group != 0;          // more than 512 inputs, or a number that 512 inputs are no multiple of
+    if (longer) p.span = p.group;
+    p.W4 = static_cast<uint8_t *>(W4); p.ldw = ldw;
+    p.s = s; p.s_bf16 = s_dtype == SQ_BF16; p.lds = lds; p.z = z; p.ldz = ldz;
+    p.groups = int((K + group - 1) / group);
+    const int64_t tiles_k = (K + p.span - 1) / p.span, blocks = tiles_k * ((N + kQuantRows - 1) / kQuantRows);
+    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    p.tiles_k = int(tiles_k);
+    auto go = [&](auto kernel) { kernel<<<unsigned(blocks), 256, 0, st>>>(p); };
+    auto lanes = [&](auto t, auto zp) {
         using Tin = decltype(t);
-        using Ts = decltype(ts);
-        if (z) quantize_w4_group_kernel<Tin, Ts, true><<<grid, 256, 0, st>>>(p);
-        else quantize_w4_group_kernel<Tin, Ts, false><<<grid, 256, 0, st>>>(p);
+        constexpr bool ZP = decltype(zp)::value;
+        if (longer) go(quantize_w4_group_kernel<Tin, ZP, 32, true>);
+        else if (p.group == 32) go(quantize_w4_group_kernel<Tin, ZP, 2, false>);
+        else if (p.group == 64) go(quantize_w4_group_kernel<Tin, ZP, 4, false>);
+        else if (p.group == 128) go(quantize_w4_group_kernel<Tin, ZP, 8, false>);
+        else if (p.group == 256) go(quantize_w4_group_kernel<Tin, ZP, 16, false>);
+        else go(quantize_w4_group_kernel<Tin, ZP, 32, false>);
     };
-    if (dt == SQ_F32) s_dtype == SQ_F32 ? go(float(), float()) : go(float(), __nv_bfloat16());
-    else s_dtype == SQ_F32 ? go(__nv_bfloat16(), float()) : go(__nv_bfloat16(), __nv_bfloat16());
+    if (dt == SQ_F32) z ? lanes(float(), std::true_type()) : lanes(float(), std::false_type());
+    else z ? lanes(__nv_bfloat16(), std::true_type()) : lanes(__nv_bfloat16(), std::false_type());
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     count_launch();
