@@ -317,7 +317,7 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     only; Y must not overlap X.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072; any M, meant for M of at most about 32
  *     (the weights are read once per pass of up to 10 rows).  No workspace.
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
- *     N <= 2097120 for segquant_dequantize_w4_group. */
+ *     N <= 4194240 for segquant_dequantize_w4_group. */
 sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *Wq4,
                                      int64_t ldw, void *s_w, sq_dtype s_dtype, int64_t lds, int8_t *z_w, int64_t ldz, void *stream);
 sq_status segquant_dequantize_w4_group(const void *Wq4, int64_t ldw, int64_t N, int64_t K, int64_t group, const void *s_w,

@@ -23,10 +23,10 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------- quantize / dequantize
 
-constexpr int kTileRows = 32;        // dequantize: channels per block
+constexpr int kTileRows = 64;        // dequantize: channels per block
 constexpr int kTileK = 256;          // .. inputs per block: 8 per lane of a warp
-constexpr int kRowsPerWarp = 4;      // .. 8 warps
-constexpr int kQuantRows = 16;       // quantize: channels per block, two per warp
+constexpr int kRowsPerWarp = 8;      // .. 8 warps
+template <typename Tin> constexpr int kWarpRows = sizeof(Tin) == 2 ? 4 : 2;      // quantize: channels per warp, 64 bytes a lane
 constexpr int kQuantK = 512;         // .. inputs per block (or one longer group): 16 per lane
 
 // elements k .. k + 7 of a row of K, zero behind its end; wide: 16 bytes at a time
@@ -56,11 +56,19 @@ __device__ __forceinline__ float stored_scale(float s, bool bf16)
     return r == 0.0f ? 1.0f : r;
 }
 
+// 32 bytes at once; the address is a multiple of 32
+__device__ __forceinline__ void load32(const void *p, uint4 &a, uint4 &b)
+{
+    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
+}
+
 struct W4QuantParams {
     const void *W;
     int64_t ld;
     int N, K;
     int group, span, tiles_k;        // span: inputs per block
+    int wide;                        // rows on 32-byte boundaries
     uint8_t *W4;
     int64_t ldw;
     void *s;
@@ -109,22 +117,35 @@ __device__ __noinline__ uint2 codes16_slow(const float *x, float s, float lo, fl
     return make_uint2(w[0], w[1]);
 }
 
-// Bound by reading W.  A warp takes 512 consecutive inputs of a channel, 16 per lane, and two channels; LANES lanes of a group agree
-// on its extrema by shuffles, and the codes leave as 256 consecutive bytes.  Groups longer than 512 (LONG) read the channel's group
-// twice, the second time from cache.  Scales and zero-points are [groups][N]; a block of 16 channels gathers them in shared memory,
-// so that they leave as runs of 16 channels.  (Eight inputs per lane and loops for any group: 43 instructions per weight, 128 us
-// for 18432 x 4608 bf16; 16 inputs and fixed lanes XX.)
+// Bound by reading W.  A warp takes 512 consecutive inputs of a channel, 16 per lane, and four channels (fp32: two), whose loads all go
+// out first; LANES lanes of a group agree on its extrema by shuffles, and the codes leave as 256 consecutive bytes.  Groups longer
+// than 512 (LONG) read the channel's group twice, the second time from cache.  Scales and zero-points are [groups][N]; a block
+// gathers those of its channels in shared memory, so that they leave as runs.  (Eight inputs per lane and loops for any group: 43
+// instructions per weight, 128 us for 18432 x 4608 bf16; 16 inputs and fixed lanes 64 us with two channels, XX with four.)
 template <typename Tin, bool ZP, int LANES, bool LONG>
 __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_constant__ W4QuantParams prm)
 {
     constexpr int G = 32 / LANES;                        // groups of a warp's inputs
-    __shared__ float sm_s[G][kQuantRows];
-    __shared__ int8_t sm_z[G][kQuantRows];
+    constexpr int ROWS = kWarpRows<Tin>, BLOCK_ROWS = 8 * ROWS, V = int(sizeof(Tin));        // V: 16-byte words of 16 inputs
+    __shared__ float sm_s[G][BLOCK_ROWS + 1];            // (a pitch that keeps the groups of a channel on different banks)
+    __shared__ int8_t sm_z[G][BLOCK_ROWS + 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tile_n = int(blockIdx.x) / prm.tiles_k, kb = (int(blockIdx.x) - tile_n * prm.tiles_k) * prm.span;
-    const int n0 = tile_n * kQuantRows + warp * 2, k0 = kb + lane * 16;
+    const int n0 = tile_n * BLOCK_ROWS + warp * ROWS, k0 = kb + lane * 16;
     const int k_end = LONG ? min(prm.K, kb + prm.span) : prm.K;
     const Tin *W = static_cast<const Tin *>(prm.W) + int64_t(n0) * prm.ld;
+    const bool inside = n0 + ROWS <= prm.N && kb + kQuantK <= k_end;     // nothing to look at
+    uint4 raw[ROWS][V];
+    if (inside) {
+#pragma unroll
+        for (int r = 0; r < ROWS; r++)
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(W + r * prm.ld + k0) + i;
+                if (prm.wide) load32(p, raw[r][i], raw[r][i + 1]);
+                else raw[r][i] = __ldg(p), raw[r][i + 1] = __ldg(p + 1);
+            }
+    }
     auto load16 = [&](int r, int k, float (&x)[16]) {
         float a[8], b[8];
         if (n0 + r < prm.N) {
@@ -137,63 +158,46 @@ __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < 8; i++) x[i] = a[i], x[i + 8] = b[i];
     };
-    float x[2][16];
-    if (n0 + 2 <= prm.N && kb + kQuantK <= k_end) {      // nothing to look at: both rows' loads in one go
-        constexpr int V = int(sizeof(Tin));              // 16-byte words of 16 inputs
-        uint4 v[2][V];
 #pragma unroll
-        for (int r = 0; r < 2; r++)
-#pragma unroll
-            for (int i = 0; i < V; i++) v[r][i] = __ldg(reinterpret_cast<const uint4 *>(W + r * prm.ld + k0) + i);
-#pragma unroll
-        for (int r = 0; r < 2; r++) {
-            const uint32_t *w = reinterpret_cast<const uint32_t *>(v[r]);
+    for (int r = 0; r < ROWS; r++) {
+        float x[16];
+        if (inside) {
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(raw[r]);
 #pragma unroll
             for (int i = 0; i < 16; i++)
-                x[r][i] = sizeof(Tin) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+                x[i] = sizeof(Tin) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        } else {
+            load16(r, k0, x);
         }
-    } else {
-        load16(0, k0, x[0]);
-        load16(1, k0, x[1]);
-    }
-    float hi[2], neg[2];                                 // extrema: of both polarities (hi, -lo), or of the magnitude
-    auto extrema = [&](int r, const float (&v)[16]) {
+        float hi = 0.0f, neg = 0.0f;                     // extrema: of both polarities (hi, -lo), or of the magnitude
+        auto extrema = [&](const float (&v)[16]) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            hi[r] = fmaxf(hi[r], ZP ? v[i] : fabsf(v[i]));
-            if (ZP) neg[r] = fmaxf(neg[r], -v[i]);
-        }
-    };
-#pragma unroll
-    for (int r = 0; r < 2; r++) {
-        hi[r] = neg[r] = 0.0f;
-        extrema(r, x[r]);
+            for (int i = 0; i < 16; i++) {
+                hi = fmaxf(hi, ZP ? v[i] : fabsf(v[i]));
+                if (ZP) neg = fmaxf(neg, -v[i]);
+            }
+        };
+        extrema(x);
         if (LONG) {
             for (int k = k0 + kQuantK; k < k_end; k += kQuantK) {
                 float more[16];
                 load16(r, k, more);
-                extrema(r, more);
+                extrema(more);
             }
         }
-    }
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) {
-#pragma unroll
-        for (int r = 0; r < 2; r++) {
-            hi[r] = fmaxf(hi[r], __shfl_xor_sync(0xFFFFFFFFu, hi[r], o));
-            if (ZP) neg[r] = fmaxf(neg[r], __shfl_xor_sync(0xFFFFFFFFu, neg[r], o));
+        for (int o = 1; o < LANES; o <<= 1) {
+            hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
+            if (ZP) neg = fmaxf(neg, __shfl_xor_sync(0xFFFFFFFFu, neg, o));
         }
-    }
-#pragma unroll
-    for (int r = 0; r < 2; r++) {
-        const float s = stored_scale(ZP ? __fdiv_rn(__fadd_rn(hi[r], neg[r]), 15.0f) : __fdiv_rn(hi[r], 7.0f), prm.s_bf16);
-        const float z = ZP ? rintf(__fdiv_rn(neg[r], s)) - 8.0f : 0.0f;   // (-8 - round(lo / s): rounding is symmetric)
+        const float s = stored_scale(ZP ? __fdiv_rn(__fadd_rn(hi, neg), 15.0f) : __fdiv_rn(hi, 7.0f), prm.s_bf16);
+        const float z = ZP ? rintf(__fdiv_rn(neg, s)) - 8.0f : 0.0f;      // (-8 - round(lo / s): rounding is symmetric)
         const SegConst c = seg_const(s);
         const float lo = (ZP ? -8.0f : -7.0f) - z, top = 7.0f - z;
         const uint32_t z4 = (uint32_t(int(z)) & 15u) * 0x01010101u;
         for (int k = k0; k < k_end; k += kQuantK) {
-            if (LONG && k != k0) load16(r, k, x[r]);
-            const uint2 w = c.fast ? codes16<ZP>(x[r], c, top, z4) : codes16_slow<ZP>(x[r], s, lo, top, z4);
+            if (LONG && k != k0) load16(r, k, x);
+            const uint2 w = c.fast ? codes16<ZP>(x, c, top, z4) : codes16_slow<ZP>(x, s, lo, top, z4);
             if (n0 + r < prm.N) {
                 uint8_t *out = prm.W4 + (n0 + r) * prm.ldw + k / 2;
                 if (k + 16 <= k_end) {
@@ -206,13 +210,13 @@ __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_con
             if (!LONG) break;
         }
         if (lane % LANES == 0) {
-            sm_s[lane / LANES][warp * 2 + r] = s;
-            if (ZP) sm_z[lane / LANES][warp * 2 + r] = int8_t(z);
+            sm_s[lane / LANES][warp * ROWS + r] = s;
+            if (ZP) sm_z[lane / LANES][warp * ROWS + r] = int8_t(z);
         }
     }
     __syncthreads();
-    if (threadIdx.x < G * kQuantRows) {
-        const int gi = threadIdx.x / kQuantRows, i = threadIdx.x % kQuantRows, g = kb / prm.group + gi, n = tile_n * kQuantRows + i;
+    for (int j = threadIdx.x; j < G * BLOCK_ROWS; j += 256) {
+        const int gi = j / BLOCK_ROWS, i = j % BLOCK_ROWS, g = kb / prm.group + gi, n = tile_n * BLOCK_ROWS + i;
         if (g < prm.groups && n < prm.N) {
             if (prm.s_bf16) static_cast<__nv_bfloat16 *>(prm.s)[g * prm.lds + n] = __float2bfloat16_rn(sm_s[gi][i]);
             else static_cast<float *>(prm.s)[g * prm.lds + n] = sm_s[gi][i];
@@ -922,10 +926,12 @@ sq_status launch_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_
     p.span = std::max(p.group, kQuantK);
     const bool longer = kQuantK % p.group != 0;          // more than 512 inputs, or a number that 512 inputs are no multiple of
     if (longer) p.span = p.group;
+    p.wide = (reinterpret_cast<uintptr_t>(W) & 31u) == 0 && ld * (dt == SQ_F32 ? 4 : 2) % 32 == 0;
     p.W4 = static_cast<uint8_t *>(W4); p.ldw = ldw;
     p.s = s; p.s_bf16 = s_dtype == SQ_BF16; p.lds = lds; p.z = z; p.ldz = ldz;
     p.groups = int((K + group - 1) / group);
-    const int64_t tiles_k = (K + p.span - 1) / p.span, blocks = tiles_k * ((N + kQuantRows - 1) / kQuantRows);
+    const int64_t block_rows = 8 * (dt == SQ_F32 ? kWarpRows<float> : kWarpRows<__nv_bfloat16>);
+    const int64_t tiles_k = (K + p.span - 1) / p.span, blocks = tiles_k * ((N + block_rows - 1) / block_rows);
     if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
     p.tiles_k = int(tiles_k);
     auto go = [&](auto kernel) { kernel<<<unsigned(blocks), 256, 0, st>>>(p); };

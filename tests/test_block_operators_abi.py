@@ -41,7 +41,7 @@ def test_group_quantizer_refusals(L, back):
     for group in (0, -32, 16, 48, 96, 192, 255, 300):
         assert q(group=group) == 5, group
     if back:
-        assert q(N=1 << 22, lds=1 << 22) == 2                   # more channel blocks than a grid has
+        assert q(N=1 << 23, lds=1 << 23) == 2                   # more channel blocks than a grid has
 
 
 def matvec(L, X=FAKE, dt=1, M=4, K=256, ldx=256, act=0, W4=2 * FAKE, ldw=128, N=64, group=64, s=3 * FAKE, sdt=0, lds=64, z=0, ldz=64,
