@@ -42,6 +42,7 @@ struct BlockNormParams {
     int vec;                          // bit i: vector i of post_w, post_b, w, b, gate, scale, shift may be read 16 bytes at a time
     int has;                          // bits: which of P, Q, A, B there are
     int sm_at[4];                     // where they lie in shared memory
+    int half;                         // floats of half a vector there
     int two_steps;                    // shared memory holds P and Q or A and B
     float alpha, eps, inv_c;
     void *H, *O;
@@ -79,19 +80,30 @@ __device__ __forceinline__ void load_chunk(const T *row, int col, int C, Chunk<T
         if (col + i * PER < C) c.v[i] = load_stream(row + col + i * PER);
     }
 }
+// eight elements as four packed pairs: most of the arithmetic goes two elements per instruction
 template <typename T>
-__device__ __forceinline__ void expand(const Chunk<T> &c, float (&x)[8])
+__device__ __forceinline__ void expand(const Chunk<T> &c, uint64_t (&x)[4])
 {
     const uint32_t *w = reinterpret_cast<const uint32_t *>(c.v);
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-        x[i] = sizeof(T) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    for (int i = 0; i < 4; i++)
+        x[i] = sizeof(T) == 4 ? pack2(__uint_as_float(w[2 * i % (2 * sizeof(T))]), __uint_as_float(w[(2 * i + 1) % (2 * sizeof(T))]))
+                              : pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
 }
-// elements behind the row's end become zero, for the sums
-__device__ __forceinline__ void cut(float (&x)[8], int left)
+__device__ __forceinline__ void singles(const uint64_t (&x)[4], float (&v)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = i < left ? x[i] : 0.0f;
+    for (int i = 0; i < 4; i++) unpack2(x[i], v[2 * i], v[2 * i + 1]);
+}
+// elements behind the row's end become zero, for the sums
+__device__ __forceinline__ void cut(uint64_t (&x)[4], int left)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        float a, b;
+        unpack2(x[i], a, b);
+        x[i] = pack2(2 * i < left ? a : 0.0f, 2 * i + 1 < left ? b : 0.0f);
+    }
 }
 template <typename T>
 __device__ __noinline__ void store_tail(T *p, int left, Eight x)
@@ -104,8 +116,10 @@ __device__ __noinline__ void store_tail(T *p, int left, Eight x)
         }
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(T *row, int col, int C, const float (&x)[8])
+__device__ __forceinline__ void store_chunk(T *row, int col, int C, const uint64_t (&pairs)[4])
 {
+    float x[8];
+    singles(pairs, x);
     if (col + 8 <= C) {
         if (sizeof(T) == 4) {
             reinterpret_cast<float4 *>(row + col)[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -144,26 +158,32 @@ __device__ __forceinline__ void vector8(const BlockNormParams &prm, const void *
             Chunk<float> c;
 #pragma unroll
             for (int i = 0; i < 2; i++) c.v[i] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(v) + at) + i);
-            expand(c, x);
+            uint64_t p[4];
+            expand(c, p);
+            singles(p, x);
         } else {
             Chunk<__nv_bfloat16> c;
             c.v[0] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(v) + at));
-            expand(c, x);
+            uint64_t p[4];
+            expand(c, p);
+            singles(p, x);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++) x[i] = i < left ? vector1(prm, v, at + i) : 0.0f;
     }
 }
-__device__ __forceinline__ void put8(float *p, const float (&x)[8])
+// A vector in shared memory is two halves, of the first and of the last four channels of every eight, so that neighbouring lanes
+// read neighbouring 16 bytes (`half`: floats of one).
+__device__ __forceinline__ void put8(float *v, int half, int col, const float (&x)[8])
 {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    *reinterpret_cast<float4 *>(v + col / 2) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4 *>(v + half + col / 2) = make_float4(x[4], x[5], x[6], x[7]);
 }
-__device__ __forceinline__ void get8(const float *p, float (&x)[8])
+__device__ __forceinline__ void get8(const float *v, int half, int col, uint64_t (&x)[4])
 {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(v + col / 2), b = *reinterpret_cast<const ulonglong2 *>(v + half + col / 2);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
 // P and Q
 __device__ __forceinline__ void make_post(const BlockNormParams &prm, float *sm, int64_t sample, int col)
@@ -180,8 +200,8 @@ __device__ __forceinline__ void make_post(const BlockNormParams &prm, float *sm,
         w[i] *= g[i];
         b[i] *= g[i];
     }
-    if (prm.has >> kP & 1) put8(sm + prm.sm_at[kP] + col, w);
-    if (prm.has >> kQ & 1) put8(sm + prm.sm_at[kQ] + col, b);
+    if (prm.has >> kP & 1) put8(sm + prm.sm_at[kP], prm.half, col, w);
+    if (prm.has >> kQ & 1) put8(sm + prm.sm_at[kQ], prm.half, col, b);
 }
 // A and B
 __device__ __forceinline__ void make_pre(const BlockNormParams &prm, float *sm, int64_t sample, int col)
@@ -199,8 +219,8 @@ __device__ __forceinline__ void make_pre(const BlockNormParams &prm, float *sm, 
         w[i] *= f;
         b[i] = fmaf(b[i], f, t[i]);
     }
-    if (prm.has >> kA & 1) put8(sm + prm.sm_at[kA] + col, w);
-    if (prm.has >> kB & 1) put8(sm + prm.sm_at[kB] + col, b);
+    if (prm.has >> kA & 1) put8(sm + prm.sm_at[kA], prm.half, col, w);
+    if (prm.has >> kB & 1) put8(sm + prm.sm_at[kB], prm.half, col, b);
 }
 
 // Sum over the WPR warps of a row, the same bits in every lane.  `red`: WPR floats of the row, another buffer each time.
@@ -220,35 +240,38 @@ __device__ __forceinline__ float row_sum(float v, float *red, int warp_of_row, i
 
 // x <- normalised x (elements behind the row's end are zero before, and do not count)
 template <int CH, int WPR>
-__device__ __forceinline__ void normalise(float (&x)[CH][8], int kind, const BlockNormParams &prm, const int (&col)[CH], float *red,
+__device__ __forceinline__ void normalise(uint64_t (&x)[CH][4], int kind, const BlockNormParams &prm, const int (&col)[CH], float *red,
                                           int warp_of_row, int row_of_block)
 {
+    float a, b;
     if (kind == SQ_NORM_LAYER) {
-        float s = 0.0f;
+        uint64_t s = 0;
 #pragma unroll
         for (int c = 0; c < CH; c++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) s += x[c][i];
-        const float mean = row_sum<WPR>(s, red, warp_of_row, row_of_block) * prm.inv_c;
+            for (int i = 0; i < 4; i++) s = add2(s, x[c][i]);
+        unpack2(s, a, b);
+        const float mean = row_sum<WPR>(a + b, red, warp_of_row, row_of_block) * prm.inv_c;
 #pragma unroll
         for (int c = 0; c < CH; c++) {
-            const float m = col[c] < prm.C ? mean : 0.0f;
+            const float m = col[c] < prm.C ? -mean : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[c][i] -= m;
+            for (int i = 0; i < 4; i++) x[c][i] = add2(x[c][i], pack2(m, m));
             if (prm.ragged) cut(x[c], prm.C - col[c]);
         }
         red += WPR;
     }
-    float q = 0.0f;
+    uint64_t q = 0;
 #pragma unroll
     for (int c = 0; c < CH; c++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) q = fmaf(x[c][i], x[c][i], q);
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR>(q, red, warp_of_row, row_of_block), prm.inv_c, prm.eps));
+        for (int i = 0; i < 4; i++) q = fma2(x[c][i], x[c][i], q);
+    unpack2(q, a, b);
+    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR>(a + b, red, warp_of_row, row_of_block), prm.inv_c, prm.eps));
 #pragma unroll
     for (int c = 0; c < CH; c++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[c][i] *= rstd;
+        for (int i = 0; i < 4; i++) x[c][i] = mul2(x[c][i], pack2(rstd, rstd));
 }
 
 // Codes of a chunk that crosses a segment bound or the row's end, or whose scale is outside the fast form: element by element.
@@ -294,6 +317,7 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
     };
 #pragma unroll
     for (int c = 0; c < CH; c++) col[c] = ((c * WPR + warp_of_row) * 32 + lane) * 8;
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
     if (m < r1) fetch(m);
 
     uint32_t seg[CODES ? CH : 1];                              // K-segment of a chunk; bit 31: it is done element by element
@@ -331,7 +355,7 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
             }
         }
         for (; m < end; m += RPB) {
-            float h[CH][8];
+            uint64_t h[CH][4];
             if (Y) {
 #pragma unroll
                 for (int c = 0; c < CH; c++) expand(y[c], h[c]);
@@ -352,25 +376,20 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
 #pragma unroll
                 for (int c = 0; c < CH; c++) {
                     if (col[c] >= C) continue;
-                    float v[8], x[8];
-                    if (R) {
-                        expand(r[c], x);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; i++) x[i] = 0.0f;
-                    }
+                    uint64_t v[4], x[4] = {0, 0, 0, 0};
+                    if (R) expand(r[c], x);
                     if (prm.has >> kQ & 1) {
-                        get8(sm + prm.sm_at[kQ] + col[c], v);
+                        get8(sm + prm.sm_at[kQ], prm.half, col[c], v);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) x[i] += v[i];
+                        for (int i = 0; i < 4; i++) x[i] = add2(x[i], v[i]);
                     }
                     if (prm.has >> kP & 1) {
-                        get8(sm + prm.sm_at[kP] + col[c], v);
+                        get8(sm + prm.sm_at[kP], prm.half, col[c], v);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) h[c][i] = fmaf(h[c][i], v[i], x[i]);
+                        for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], x[i]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 8; i++) h[c][i] += x[i];
+                        for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], x[i]);
                     }
                 }
             } else {
@@ -401,16 +420,20 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
 #pragma unroll
                 for (int c = 0; c < CH; c++) {
                     if (col[c] >= C) continue;
-                    float v[8];
-                    if (prm.has >> kA & 1) {
-                        get8(sm + prm.sm_at[kA] + col[c], v);
+                    uint64_t v[4], w[4];
+                    if ((prm.has >> kA & 3) == 3) {
+                        get8(sm + prm.sm_at[kA], prm.half, col[c], v);
+                        get8(sm + prm.sm_at[kB], prm.half, col[c], w);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) h[c][i] *= v[i];
-                    }
-                    if (prm.has >> kB & 1) {
-                        get8(sm + prm.sm_at[kB] + col[c], v);
+                        for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], w[i]);
+                    } else if (prm.has >> kA & 1) {
+                        get8(sm + prm.sm_at[kA], prm.half, col[c], v);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) h[c][i] += v[i];
+                        for (int i = 0; i < 4; i++) h[c][i] = mul2(h[c][i], v[i]);
+                    } else if (prm.has >> kB & 1) {
+                        get8(sm + prm.sm_at[kB], prm.half, col[c], v);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], v[i]);
                     }
                     if (!CODES) {
                         store_chunk(static_cast<T *>(prm.O) + m * prm.ldo, col[c], C, h[c]);
@@ -418,12 +441,13 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
                         uint8_t *dp = prm.c_pos + m * prm.ldc + col[c], *dn = DUAL ? prm.c_neg + m * prm.ldc + col[c] : nullptr;
                         if (seg[c] >> 31) {
                             Eight e;
-#pragma unroll
-                            for (int i = 0; i < 8; i++) e.v[i] = h[c][i];
+                            singles(h[c], e.v);
                             codes_tail<CODE, MODE>(prm, col[c], e, dp, dn);
                         } else {
                             const SegConst cp = sm_pos[seg[c]], cn = DUAL ? sm_neg[seg[c]] : cp;
-                            const float a[4] = {h[c][0], h[c][1], h[c][2], h[c][3]}, b[4] = {h[c][4], h[c][5], h[c][6], h[c][7]};
+                            float a[4], b[4];
+                            unpack2(h[c][0], a[0], a[1]), unpack2(h[c][1], a[2], a[3]);
+                            unpack2(h[c][2], b[0], b[1]), unpack2(h[c][3], b[2], b[3]);
                             uint32_t wp[2], wn[2];
                             quant4<CODE, MODE>(a, cp, cn, float(prm.hi), 0, wp[0], wn[0]);
                             quant4<CODE, MODE>(b, cp, cn, float(prm.hi), 0, wp[1], wn[1]);
@@ -453,6 +477,7 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     auto go = [&](auto kernel, int wpr, int rpb) {
         const int threads = wpr * rpb * 32;
         int vectors = 0;
+        p.half = pitch / 2;
         for (int i = 0; i < 4; i++)
             if (p.has >> i & 1) p.sm_at[i] = pitch * vectors++;
         if (rpb == 1 && vectors == 4 && 4 * pitch * 4 > kMaxVectorBytes) {      // then two at a time, made anew for every row
@@ -467,8 +492,18 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
         }
         const int per_sm = rpb > 1 ? 2 : std::max(1, std::min(1024 / threads, int(kMaxVectorBytes / (smem + 1024))));
         const int64_t blocks = std::min<int64_t>((p.M + rpb - 1) / rpb, int64_t(sms) * per_sm);
-        kernel<<<unsigned(blocks), threads, smem, st>>>(p);
-        const cudaError_t e = cudaGetLastError();
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(unsigned(blocks));
+        cfg.blockDim = dim3(unsigned(threads));
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        void *args[1] = {&p};
+        const cudaError_t e = cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), args);
         if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
         count_launch();
         return SQ_OK;
