@@ -292,8 +292,9 @@ __device__ __noinline__ void codes_tail(const BlockNormParams &prm, int col, Eig
 
 // Threads of a block: RPB rows at a time, WPR warps each.  RPB > 1: the block's rows share the vectors of their sample in shared memory;
 // RPB == 1: every thread makes and reads those of its own channels, so nothing has to wait.
-template <typename T, int OUT, int CH, int WPR, int RPB>
-__global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
+// BLOCKS: resident blocks per SM that the registers are held to.
+template <typename T, int OUT, int CH, int WPR, int RPB, int BLOCKS>
+__global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
 {
     constexpr bool CODES = OUT != kOutValues, DUAL = OUT == kOutInt8Dual || OUT == kOutE4m3Dual, SHARED = RPB > 1;
     constexpr int CODE = OUT >= kOutE4m3 ? SQ_CODE_E4M3 : SQ_CODE_INT8, MODE = DUAL ? kDual : kSingle;
@@ -464,9 +465,10 @@ __global__ void __launch_bounds__(WPR * RPB * 32, RPB > 1 ? 2 : 1) block_norm_ke
     }
 }
 
-// One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1536 bf16 (1024 fp32) channels
-// where there are rows enough for that, two and four up to four times as many, then a block per row; few rows get a block each, and
-// so do rows that each have vectors of their own.
+// One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1280 bf16 (1024 fp32) channels
+// where there are rows enough for that, two and four up to 4096, then a block per row; few rows get a block each, and so do rows that have
+// vectors of their own.  (8858 x 1536 bf16 to codes: one warp with six chunks a lane, held to 128 registers, 28.1 us; two with three
+// 23.1 us.  32768 x 1280: one warp with five chunks 55.8 us, two with three, of which one sixth is idle, 63.2 us.)
 template <typename T, int OUT>
 sq_status run_shape(BlockNormParams p, cudaStream_t st)
 {
@@ -474,7 +476,7 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return SQ_ERR_CUDA;
     const int pitch = (p.C + 7) / 8 * 8;                 // floats of a vector in shared memory
-    auto go = [&](auto kernel, int wpr, int rpb) {
+    auto go = [&](auto kernel, int wpr, int rpb, int shared_blocks) {
         const int threads = wpr * rpb * 32;
         int vectors = 0;
         p.half = pitch / 2;
@@ -490,7 +492,7 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
             const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxVectorBytes);
             if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
         }
-        const int per_sm = rpb > 1 ? 2 : std::max(1, std::min(1024 / threads, int(kMaxVectorBytes / (smem + 1024))));
+        const int per_sm = rpb > 1 ? shared_blocks : std::max(1, std::min(1024 / threads, int(kMaxVectorBytes / (smem + 1024))));
         const int64_t blocks = std::min<int64_t>((p.M + rpb - 1) / rpb, int64_t(sms) * per_sm);
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3(unsigned(blocks));
@@ -510,26 +512,26 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     };
     const int chunks = (p.C + 7) / 8;
     constexpr bool HALF = sizeof(T) == 2;
-#define SQ_SHAPE(CH, WPR, RPB) return go(block_norm_kernel<T, OUT, CH, WPR, RPB>, WPR, RPB)
+#define SQ_SHAPE(CH, WPR, RPB, BLOCKS) return go(block_norm_kernel<T, OUT, CH, WPR, RPB, BLOCKS>, WPR, RPB, BLOCKS)
     if (p.M >= int64_t(sms) * 8 && p.rows_per_sample >= 16) {
-        if (chunks <= 32) SQ_SHAPE(1, 1, 8);
-        if (chunks <= 64) SQ_SHAPE(2, 1, 8);
-        if (chunks <= 96) SQ_SHAPE(3, 1, 8);
-        if (chunks <= 128) SQ_SHAPE(4, 1, 8);
+        if (chunks <= 32) SQ_SHAPE(1, 1, 8, 2);
+        if (chunks <= 64) SQ_SHAPE(2, 1, 8, 2);
+        if (chunks <= 96) SQ_SHAPE(3, 1, 8, 2);
+        if (chunks <= 128) SQ_SHAPE(4, 1, 8, 2);
         if constexpr (HALF) {
-            if (chunks <= 160) SQ_SHAPE(5, 1, 8);
-            if (chunks <= 192) SQ_SHAPE(6, 1, 8);
+            if (chunks <= 160) SQ_SHAPE(5, 1, 8, 2);
+            if (chunks <= 192) SQ_SHAPE(3, 2, 4, 3);
         } else {
-            if (chunks <= 192) SQ_SHAPE(3, 2, 4);
+            if (chunks <= 192) SQ_SHAPE(3, 2, 4, 2);
         }
-        if (chunks <= 256) SQ_SHAPE(4, 2, 4);
-        if (chunks <= 512) SQ_SHAPE(4, 4, 2);
+        if (chunks <= 256) SQ_SHAPE(4, 2, 4, 2);
+        if (chunks <= 512) SQ_SHAPE(4, 4, 2, 2);
     }
-    if (chunks <= 128) SQ_SHAPE(1, 4, 1);
-    if (chunks <= 256) SQ_SHAPE(2, 4, 1);
-    if (chunks <= 512) SQ_SHAPE(2, 8, 1);
-    if (chunks <= 1024) SQ_SHAPE(4, 8, 1);
-    if (chunks <= 2048) SQ_SHAPE(4, 16, 1);
+    if (chunks <= 128) SQ_SHAPE(1, 4, 1, 1);
+    if (chunks <= 256) SQ_SHAPE(2, 4, 1, 1);
+    if (chunks <= 512) SQ_SHAPE(2, 8, 1, 1);
+    if (chunks <= 1024) SQ_SHAPE(4, 8, 1, 1);
+    if (chunks <= 2048) SQ_SHAPE(4, 16, 1, 1);
 #undef SQ_SHAPE
     return SQ_ERR_UNSUPPORTED;
 }

@@ -112,7 +112,8 @@ PyObject *guarded(const char *name, Py_ssize_t n, Py_ssize_t want, F f)
 // code matrix [rows, K] with a 128-byte padded row pitch, as binding.new_codes makes it
 at::Tensor new_codes(int64_t rows, int64_t K, const at::Tensor &like)
 {
-    return at::empty({rows, (K + 127) / 128 * 128}, like.options().dtype(at::kByte)).narrow(1, 0, K);
+    const at::Tensor t = at::empty({rows, (K + 127) / 128 * 128}, like.options().dtype(at::kByte));
+    return K % 128 ? t.narrow(1, 0, K) : t;
 }
 
 // X, Wq, seg, code, s_pos, s_neg, s_w, bias, Y, scratch, workspace, x_stage, y_stage, flags
@@ -343,7 +344,8 @@ float *f32_vector(const Args &a, int i, int64_t n, const char *what)
 // [rows, cols] with rows on boundaries of 16 bytes (and of 16 elements)
 at::Tensor new_rows(int64_t rows, int64_t cols, const at::Tensor &like, at::ScalarType type)
 {
-    return at::empty({rows, (cols + 15) / 16 * 16}, like.options().dtype(type)).narrow(1, 0, cols);
+    const at::Tensor t = at::empty({rows, (cols + 15) / 16 * 16}, like.options().dtype(type));
+    return cols % 16 ? t.narrow(1, 0, cols) : t;
 }
 
 struct GroupScales {
