@@ -43,6 +43,7 @@ struct BlockNormParams {
     int has;                          // bits: which of P, Q, A, B there are
     int sm_at[4];                     // where they lie in shared memory
     int half;                         // floats of half a vector there
+    int own;                          // floats of a row's own vectors there (0: rows share them)
     int two_steps;                    // shared memory holds P and Q or A and B
     float alpha, eps, inv_c;
     void *H, *O;
@@ -223,23 +224,31 @@ __device__ __forceinline__ void make_pre(const BlockNormParams &prm, float *sm, 
     if (prm.has >> kB & 1) put8(sm + prm.sm_at[kB], prm.half, col, b);
 }
 
-// Sum over the WPR warps of a row, the same bits in every lane.  `red`: WPR floats of the row, another buffer each time.
-template <int WPR>
+// Sum over the WPR warps (the L lanes) of a row, the same bits in every lane.  `red`: WPR floats of the row, another buffer each time.
+template <int WPR, int L>
 __device__ __forceinline__ float row_sum(float v, float *red, int warp_of_row, int row_of_block)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     if (WPR == 1) return v;
     if ((threadIdx.x & 31) == 0) red[warp_of_row] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(row_of_block + 1), "n"(WPR * 32) : "memory");
     v = 0.0f;
+    if (WPR % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < WPR; i++) v += red[i];
+        for (int i = 0; i < WPR; i += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(red + i);
+            v += f.x + f.y + f.z + f.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < WPR; i++) v += red[i];
+    }
     return v;
 }
 
 // x <- normalised x (elements behind the row's end are zero before, and do not count)
-template <int CH, int WPR>
+template <int CH, int WPR, int L>
 __device__ __forceinline__ void normalise(uint64_t (&x)[CH][4], int kind, const BlockNormParams &prm, const int (&col)[CH], float *red,
                                           int warp_of_row, int row_of_block)
 {
@@ -251,7 +260,7 @@ __device__ __forceinline__ void normalise(uint64_t (&x)[CH][4], int kind, const 
 #pragma unroll
             for (int i = 0; i < 4; i++) s = add2(s, x[c][i]);
         unpack2(s, a, b);
-        const float mean = row_sum<WPR>(a + b, red, warp_of_row, row_of_block) * prm.inv_c;
+        const float mean = row_sum<WPR, L>(a + b, red, warp_of_row, row_of_block) * prm.inv_c;
 #pragma unroll
         for (int c = 0; c < CH; c++) {
             const float m = col[c] < prm.C ? -mean : 0.0f;
@@ -267,7 +276,7 @@ __device__ __forceinline__ void normalise(uint64_t (&x)[CH][4], int kind, const 
 #pragma unroll
         for (int i = 0; i < 4; i++) q = fma2(x[c][i], x[c][i], q);
     unpack2(q, a, b);
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR>(a + b, red, warp_of_row, row_of_block), prm.inv_c, prm.eps));
+    const float rstd = 1.0f / sqrtf(fmaf(row_sum<WPR, L>(a + b, red, warp_of_row, row_of_block), prm.inv_c, prm.eps));
 #pragma unroll
     for (int c = 0; c < CH; c++)
 #pragma unroll
@@ -290,23 +299,27 @@ __device__ __noinline__ void codes_tail(const BlockNormParams &prm, int col, Eig
     }
 }
 
-// Threads of a block: RPB rows at a time, WPR warps each.  RPB > 1: the block's rows share the vectors of their sample in shared memory;
-// RPB == 1: every thread makes and reads those of its own channels, so nothing has to wait.
-// BLOCKS: resident blocks per SM that the registers are held to.
-template <typename T, int OUT, int CH, int WPR, int RPB, int BLOCKS>
-__global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
+// Threads of a block: RPB rows at a time, WPR warps each, or L = 8 or 16 lanes for rows of at most 64 and 128 channels.  A block's rows share the
+// vectors of their sample in shared memory; with OWN vectors (a block per row, or samples of few rows) every thread makes and
+// reads those of its own channels, so nothing has to wait.  BLOCKS: resident blocks per SM that the registers are held to.
+template <typename T, int OUT, int CH, int WPR, int RPB, int BLOCKS, bool OWN, int L = 32>
+__global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const __grid_constant__ BlockNormParams prm)
 {
-    constexpr bool CODES = OUT != kOutValues, DUAL = OUT == kOutInt8Dual || OUT == kOutE4m3Dual, SHARED = RPB > 1;
+    static_assert(OWN || RPB > 1, "rows to share with");
+    static_assert(L == 32 || (WPR == 1 && CH == 1), "rows of a few lanes");
+    constexpr bool CODES = OUT != kOutValues, DUAL = OUT == kOutInt8Dual || OUT == kOutE4m3Dual;
     constexpr int CODE = OUT >= kOutE4m3 ? SQ_CODE_E4M3 : SQ_CODE_INT8, MODE = DUAL ? kDual : kSingle;
     extern __shared__ __align__(16) float sm[];
     __shared__ SegConst sm_pos[CODES ? SQ_MAX_P : 1], sm_neg[CODES && DUAL ? SQ_MAX_P : 1];
-    __shared__ float sm_red[WPR > 1 ? RPB * 4 * WPR : 1];       // four sums a row: mean and variance, twice
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row_of_block = warp / WPR, warp_of_row = warp % WPR;
+    __shared__ __align__(16) float sm_red[WPR > 1 ? RPB * 4 * WPR : 1];       // four sums a row: mean and variance, twice
+    const int lane = threadIdx.x & (L - 1), warp = threadIdx.x >> 5, row_of_block = threadIdx.x / (WPR * L), warp_of_row = warp % WPR;
+    const int of_warp = L < 32 ? (threadIdx.x & 31) / L : 0;     // which of its warp's rows
     const int C = prm.C;
+    float *vec = sm + (OWN && RPB > 1 ? row_of_block * prm.own : 0);
     const T *Y = static_cast<const T *>(prm.Y), *R = static_cast<const T *>(prm.R);
     // this block's rows, and its row group's first
     const int r0 = int(int64_t(blockIdx.x) * prm.M / gridDim.x), r1 = int((int64_t(blockIdx.x) + 1) * prm.M / gridDim.x);
-    int m = r0 + row_of_block;
+    int m = r0 + row_of_block, sample = -1;
     int col[CH];
     Chunk<T> y[CH], r[CH];
     auto fetch = [&](int row) {
@@ -317,7 +330,7 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
         }
     };
 #pragma unroll
-    for (int c = 0; c < CH; c++) col[c] = ((c * WPR + warp_of_row) * 32 + lane) * 8;
+    for (int c = 0; c < CH; c++) col[c] = ((c * WPR + warp_of_row) * L + lane) * 8;
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
     if (m < r1) fetch(m);
 
@@ -338,24 +351,33 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
         }
     }
     float *red = sm_red + (WPR > 1 ? row_of_block * 4 * WPR : 0);
-    int start = r0;
-    for (int sample = r0 / prm.rows_per_sample; start < r1; sample++) {
-        const int end = int(min(int64_t(r1), (int64_t(sample) + 1) * prm.rows_per_sample));
-        if (SHARED) {
+    for (int start = r0, end; start < r1; start = end) {
+        end = r1;
+        if (!OWN) {                                            // the rows of one sample
+            sample = start / prm.rows_per_sample;
+            end = int(min(int64_t(r1), (int64_t(sample) + 1) * prm.rows_per_sample));
             if (start != r0) __syncthreads();                  // the last sample's vectors have been used
             for (int k = int(threadIdx.x) * 8; k < C; k += int(blockDim.x) * 8) {
-                make_post(prm, sm, sample, k);
-                make_pre(prm, sm, sample, k);
+                make_post(prm, vec, sample, k);
+                make_pre(prm, vec, sample, k);
             }
             __syncthreads();
-        } else if (!prm.two_steps) {
-#pragma unroll 1
-            for (int c = 0; c < CH; c++) {
-                const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
-                if (k < C) make_post(prm, sm, sample, k), make_pre(prm, sm, sample, k);
+            if (L < 32 && start != r0) {                       // (rows that share a warp start a sample together)
+                m = start + row_of_block;
+                if (m < r1) fetch(m);
             }
         }
-        for (; m < end; m += RPB) {
+        for (; m - of_warp < end; m += RPB) {                  // whole warps
+            const bool valid = L == 32 || m < end;
+            if (OWN && !prm.two_steps && valid && m / prm.rows_per_sample != sample) {
+                sample = m / prm.rows_per_sample;
+#pragma unroll 1
+                for (int c = 0; c < CH; c++) {
+                    const int k = ((c * WPR + warp_of_row) * L + lane) * 8;
+                    if (k < C) make_post(prm, vec, sample, k), make_pre(prm, vec, sample, k);
+                }
+            }
+            if (OWN && RPB == 1 && prm.two_steps) sample = m / prm.rows_per_sample;
             uint64_t h[CH][4];
             if (Y) {
 #pragma unroll
@@ -365,13 +387,13 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
 #pragma unroll
                         for (int c = 0; c < CH; c++) cut(h[c], C - col[c]);
                     }
-                    normalise<CH, WPR>(h, prm.post, prm, col, red, warp_of_row, row_of_block);
+                    normalise<CH, WPR, L>(h, prm.post, prm, col, red, warp_of_row, row_of_block);
                 }
-                if (!SHARED && prm.two_steps) {
+                if (RPB == 1 && prm.two_steps) {
 #pragma unroll 1
                     for (int c = 0; c < CH; c++) {
-                        const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
-                        if (k < C) make_post(prm, sm, sample, k);
+                        const int k = ((c * WPR + warp_of_row) * L + lane) * 8;
+                        if (k < C) make_post(prm, vec, sample, k);
                     }
                 }
 #pragma unroll
@@ -380,12 +402,12 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
                     uint64_t v[4], x[4] = {0, 0, 0, 0};
                     if (R) expand(r[c], x);
                     if (prm.has >> kQ & 1) {
-                        get8(sm + prm.sm_at[kQ], prm.half, col[c], v);
+                        get8(vec + prm.sm_at[kQ], prm.half, col[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) x[i] = add2(x[i], v[i]);
                     }
                     if (prm.has >> kP & 1) {
-                        get8(sm + prm.sm_at[kP], prm.half, col[c], v);
+                        get8(vec + prm.sm_at[kP], prm.half, col[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], x[i]);
                     } else {
@@ -402,7 +424,7 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
             if (prm.H) {
 #pragma unroll
                 for (int c = 0; c < CH; c++)
-                    if (col[c] < C) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
+                    if (valid && col[c] < C) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
             }
             if (CODES || prm.O) {
                 if (prm.ragged) {
@@ -410,29 +432,29 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
                     for (int c = 0; c < CH; c++) cut(h[c], C - col[c]);
                 }
                 if (prm.pre != SQ_NORM_NONE)
-                    normalise<CH, WPR>(h, prm.pre, prm, col, red + 2 * WPR * (WPR > 1), warp_of_row, row_of_block);
-                if (!SHARED && prm.two_steps) {
+                    normalise<CH, WPR, L>(h, prm.pre, prm, col, red + 2 * WPR * (WPR > 1), warp_of_row, row_of_block);
+                if (RPB == 1 && prm.two_steps) {
 #pragma unroll 1
                     for (int c = 0; c < CH; c++) {
-                        const int k = ((c * WPR + warp_of_row) * 32 + lane) * 8;
-                        if (k < C) make_pre(prm, sm, sample, k);
+                        const int k = ((c * WPR + warp_of_row) * L + lane) * 8;
+                        if (k < C) make_pre(prm, vec, sample, k);
                     }
                 }
 #pragma unroll
                 for (int c = 0; c < CH; c++) {
-                    if (col[c] >= C) continue;
+                    if (!valid || col[c] >= C) continue;
                     uint64_t v[4], w[4];
                     if ((prm.has >> kA & 3) == 3) {
-                        get8(sm + prm.sm_at[kA], prm.half, col[c], v);
-                        get8(sm + prm.sm_at[kB], prm.half, col[c], w);
+                        get8(vec + prm.sm_at[kA], prm.half, col[c], v);
+                        get8(vec + prm.sm_at[kB], prm.half, col[c], w);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], w[i]);
                     } else if (prm.has >> kA & 1) {
-                        get8(sm + prm.sm_at[kA], prm.half, col[c], v);
+                        get8(vec + prm.sm_at[kA], prm.half, col[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = mul2(h[c][i], v[i]);
                     } else if (prm.has >> kB & 1) {
-                        get8(sm + prm.sm_at[kB], prm.half, col[c], v);
+                        get8(vec + prm.sm_at[kB], prm.half, col[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], v[i]);
                     }
@@ -461,7 +483,6 @@ __global__ void __launch_bounds__(WPR * RPB * 32, BLOCKS) block_norm_kernel(cons
             // the next row's first sums overwrite words that a slower warp may still be reading
             if (WPR > 1) asm volatile("bar.sync %0, %1;" ::"r"(row_of_block + 1), "n"(WPR * 32) : "memory");
         }
-        start = end;
     }
 }
 
@@ -476,23 +497,29 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return SQ_ERR_CUDA;
     const int pitch = (p.C + 7) / 8 * 8;                 // floats of a vector in shared memory
-    auto go = [&](auto kernel, int wpr, int rpb, int shared_blocks) {
-        const int threads = wpr * rpb * 32;
-        int vectors = 0;
-        p.half = pitch / 2;
-        for (int i = 0; i < 4; i++)
-            if (p.has >> i & 1) p.sm_at[i] = pitch * vectors++;
-        if (rpb == 1 && vectors == 4 && 4 * pitch * 4 > kMaxVectorBytes) {      // then two at a time, made anew for every row
+    int vectors = 0;
+    p.half = pitch / 2;
+    for (int i = 0; i < 4; i++)
+        if (p.has >> i & 1) p.sm_at[i] = pitch * vectors++;
+    // samples of few rows: every row has its own vectors, where shared memory has room for that
+    const bool few_a_sample = p.rows_per_sample < 16;
+    auto go = [&](auto kernel, int threads, int rpb, int blocks_per_sm) {
+        size_t smem = size_t(vectors) * pitch * 4;
+        if (rpb == 1 && smem > kMaxVectorBytes) {        // all four, over 14080 channels: two at a time then, made anew for every row
             p.two_steps = 1;
             p.sm_at[kA] = 0, p.sm_at[kB] = pitch;
-            vectors = 2;
+            smem /= 2;
         }
-        const size_t smem = size_t(vectors) * pitch * 4;
-        if (smem > 48 * 1024) {
+        if (rpb > 1 && few_a_sample) {
+            p.own = vectors * pitch;
+            smem *= rpb;
+        }
+        if (smem > 40 * 1024) {                          // (the kernel has a few KB of its own)
             const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxVectorBytes);
             if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
         }
-        const int per_sm = rpb > 1 ? shared_blocks : std::max(1, std::min(1024 / threads, int(kMaxVectorBytes / (smem + 1024))));
+        const int fit = int(kMaxVectorBytes / (smem + 4096));
+        const int per_sm = std::max(1, std::min(blocks_per_sm, fit));
         const int64_t blocks = std::min<int64_t>((p.M + rpb - 1) / rpb, int64_t(sms) * per_sm);
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3(unsigned(blocks));
@@ -512,27 +539,39 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     };
     const int chunks = (p.C + 7) / 8;
     constexpr bool HALF = sizeof(T) == 2;
-#define SQ_SHAPE(CH, WPR, RPB, BLOCKS) return go(block_norm_kernel<T, OUT, CH, WPR, RPB, BLOCKS>, WPR, RPB, BLOCKS)
-    if (p.M >= int64_t(sms) * 8 && p.rows_per_sample >= 16) {
-        if (chunks <= 32) SQ_SHAPE(1, 1, 8, 2);
-        if (chunks <= 64) SQ_SHAPE(2, 1, 8, 2);
-        if (chunks <= 96) SQ_SHAPE(3, 1, 8, 2);
-        if (chunks <= 128) SQ_SHAPE(4, 1, 8, 2);
+#define SQ_SHARED(CH, WPR, RPB, BLOCKS, L)                                                                                  \
+    return few_a_sample ? go(block_norm_kernel<T, OUT, CH, WPR, RPB, BLOCKS, true, L>, WPR * RPB * L, RPB, BLOCKS)          \
+                        : go(block_norm_kernel<T, OUT, CH, WPR, RPB, BLOCKS, false, L>, WPR * RPB * L, RPB, BLOCKS)
+#define SQ_ROW(CH, WPR, BLOCKS) return go(block_norm_kernel<T, OUT, CH, WPR, 1, BLOCKS, true>, WPR * 32, 1, BLOCKS)
+    if (p.M >= int64_t(sms) * 5 && (!few_a_sample || size_t(vectors) * pitch * 4 * 8 <= size_t(kMaxVectorBytes))) {
+        if (chunks <= 8) SQ_SHARED(1, 1, 32, 4, 8);
+        if (chunks <= 16) SQ_SHARED(1, 1, 16, 4, 16);
+        if (chunks <= 32) SQ_SHARED(1, 1, 8, 4, 32);
+        if (chunks <= 64) SQ_SHARED(2, 1, 8, HALF ? 4 : 3, 32);
+        if (chunks <= 96) SQ_SHARED(3, 1, 8, HALF ? 3 : 2, 32);
+        if (chunks <= 128) SQ_SHARED(4, 1, 8, 2, 32);
         if constexpr (HALF) {
-            if (chunks <= 160) SQ_SHAPE(5, 1, 8, 2);
-            if (chunks <= 192) SQ_SHAPE(3, 2, 4, 3);
-        } else {
-            if (chunks <= 192) SQ_SHAPE(3, 2, 4, 2);
+            if (chunks <= 160) SQ_SHARED(5, 1, 8, 2, 32);
         }
-        if (chunks <= 256) SQ_SHAPE(4, 2, 4, 2);
-        if (chunks <= 512) SQ_SHAPE(4, 4, 2, 2);
+        if (chunks <= 192) SQ_SHARED(3, 2, 4, HALF ? 3 : 2, 32);
+        if (chunks <= 256) SQ_SHARED(4, 2, 4, 2, 32);
+        if (chunks <= 512) SQ_SHARED(4, 4, 2, 2, 32);
     }
-    if (chunks <= 128) SQ_SHAPE(1, 4, 1, 1);
-    if (chunks <= 256) SQ_SHAPE(2, 4, 1, 1);
-    if (chunks <= 512) SQ_SHAPE(2, 8, 1, 1);
-    if (chunks <= 1024) SQ_SHAPE(4, 8, 1, 1);
-    if (chunks <= 2048) SQ_SHAPE(4, 16, 1, 1);
-#undef SQ_SHAPE
+    if (p.M >= int64_t(sms) * 2) {
+        if (chunks <= 128) SQ_ROW(1, 4, 6);
+        if (chunks <= 256) SQ_ROW(2, 4, 4);
+        if (chunks <= 512) SQ_ROW(2, 8, 2);
+        if (chunks <= 768) SQ_ROW(3, 8, HALF ? 3 : 2);
+        if (chunks <= 1024) SQ_ROW(4, 8, 2);
+        SQ_ROW(4, 16, 1);
+    }
+    if (chunks <= 128) SQ_ROW(1, 4, 6);
+    if (chunks <= 256) SQ_ROW(1, 8, 2);
+    if (chunks <= 512) SQ_ROW(1, 16, 1);
+    if (chunks <= 1024) SQ_ROW(1, 32, 1);
+    if (chunks <= 2048) SQ_ROW(2, 32, 1);
+#undef SQ_SHARED
+#undef SQ_ROW
     return SQ_ERR_UNSUPPORTED;
 }
 

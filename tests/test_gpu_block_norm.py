@@ -162,6 +162,19 @@ CASES = [
     (2500, 1536, 1250, BF, F32, "rms", "rms", ("post_w", "w"), True, True, False),
     (1190, 1543, 100, BF, BF, "none", "layer", ("scale", "shift"), False, True, False),
     (5000, 40, 7, F32, F32, "layer", "layer", ALL, True, True, True),
+    # rows of a few lanes, samples that end inside a warp or a block; vectors of every row
+    (5003, 64, 100, BF, BF, "rms", "layer", ALL, True, True, False),
+    (3001, 128, 1, F32, F32, "none", "layer", ("gate", "scale", "shift"), True, True, False),
+    (3000, 100, 17, BF, F32, "layer", "rms", ALL, True, True, True),
+    (40000, 8, 40000, BF, BF, "none", "rms", ("w",), True, False, False),
+    (1190, 640, 1, BF, BF, "rms", "layer", ALL, True, True, False),
+    (1300, 1300, 3, F32, BF, "layer", "layer", ALL, True, True, False),
+    # wider rows, many of them
+    (1200, 4096, 64, BF, BF, "none", "layer", ("gate", "scale", "shift"), True, True, False),
+    (1190, 2000, 16, F32, F32, "layer", "layer", ALL, True, True, False),
+    (1184, 3080, 1184, BF, BF, "rms", "rms", ("post_w", "w"), True, True, False),
+    (1184, 1500, 592, BF, BF, "layer", "layer", ALL, True, True, False),
+    (1250, 6000, 1250, BF, BF, "rms", "rms", ("post_w", "w"), True, True, False),
 ]
 
 
