@@ -346,7 +346,7 @@ struct MatvecParams {
     int tiles_round;                 // tiles whose sums fit in shared memory
     int cols, cols8;                 // columns in use, 3 * rows; rounded up to whole MMAs
     int stages;
-    uint32_t stage_bytes, z_off, x_off, f_off, xs_off, red_off, head_off;
+    uint32_t stage_bytes, z_off, x_off, f_off, xs_off, red_off, head_off, out_off;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -419,6 +419,15 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// log2 of the lanes that put an output together: a tile lies in about 16 / tiles runs, and all threads together go through the
+// outputs once
+__device__ __forceinline__ int lanes_of_output(int tiles, int outs)
+{
+    int share = tiles >= 16 ? 0 : tiles >= 8 ? 1 : tiles >= 4 ? 2 : tiles >= 2 ? 3 : 4;
+    while (share > 0 && outs << share > kWarps * 32) share--;
+    return share;
+}
+
 // A CTA of 16 warps holds its share of the activations in shared memory as MMA operands.  Its work is a list of units, 16 channels x 256 codes,
 // tile after tile of 16 channels, and every warp takes an equal run of that list: whole tiles, and the end of one and the start of
 // another.  So no warp waits for another until all of them are done, whatever the number of channels and inputs (one tile at a time, K shared by
@@ -466,6 +475,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
 
+    if (cl > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     // raw activations: what a thread converts, kAhead times eight inputs in flight.  Eight e of row m: inputs u_first kUnitK + 8 e ..
     const int eights = U * (kUnitK / 8), all_eights = eights * rows;
     struct Place {
@@ -498,10 +508,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         }
     };
     fetch();
-    // the bias of this thread's first output
+    // the bias of this thread's first output, as far as that can be told before the tiles are split
+    const int tiles0 = min(prm.tiles_round, t_last - t_first);
+    const int out0 = cl > 1 ? tid * cl + rank : tid >> lanes_of_output(tiles0, tiles0 * kTileN * rows);
     float bias0 = 0.0f;
+    const uint32_t per_row = 0xFFFFFFFFu / uint32_t(rows) + 1u;      // x / rows = the upper half of x times this, for x < 2^28 and rows > 1
+    auto tile_of = [&](int q) { return rows == 1 ? q : int(__umulhi(uint32_t(q), per_row)); };
     if (prm.bias) {
-        const int n = (t_first + (rows == 1 ? (tid * cl + rank) >> 4 : ((tid * cl + rank) >> 4) / rows)) * kTileN + ((tid * cl + rank) & 15);
+        const int n = (t_first + tile_of(out0 >> 4)) * kTileN + (out0 & 15);
         if (n < prm.N) bias0 = __ldg(prm.bias + n);
     }
 
@@ -726,40 +740,58 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 to = red + tile * (prm.cols * kRedPitch);
             }
         }
-        if (cl > 1) cluster_barrier();
-        else __syncthreads();
+        __syncthreads();
+        if (cl > 1 && t0 == t_first) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA is there to be written to
 
-        // ---- outputs: the CTAs of a cluster take turns; every sum runs over ranks, runs and an activation's bytes in this order
-        const int outs = nt_round * kTileN * rows;
-        for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
-            const int c = o & 15, q = o >> 4, tl = rows == 1 ? q : q / rows, m = q - tl * rows, n = (t0 + tl) * kTileN + c;
-            if (n >= prm.N) continue;
-            float v = bias0;
-            if (prm.bias && (t0 != t_first || o >= kWarps * 32 * cl)) v = __ldg(prm.bias + n);
-            for (int r = 0; r < cl; r++) {
-                const int Ur = min(prm.units - r * prm.units_cta, prm.units_cta), sum_units = nt_round * Ur;
-                if (Ur <= 0) break;
-                // the runs that units tl Ur .. tl Ur + Ur - 1 lie in
-                const int w_first = ((tl * Ur + 1) * kWarps - 1) / sum_units, w_last = ((tl * Ur + Ur) * kWarps - 1) / sum_units;
-                for (int w = w_first; w <= w_last; w++) {
-                    if (w * sum_units / kWarps == (w + 1) * sum_units / kWarps) continue;     // a run of nothing (fewer units than warps)
-                    const float *from = (w == w_first ? red + tl * (prm.cols * kRedPitch) : head + w * (prm.cols * kRedPitch)) + m * kRedPitch + c;
-                    uint32_t at = smem_addr(from);
-                    if (cl > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(r));
-#pragma unroll
-                    for (int p = 0; p < 3; p++) {
-                        float f;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at + p * prm.rows * kRedPitch * 4) : "memory");
-                        v += f;
-                    }
-                }
-            }
+        // ---- outputs.  2^share lanes put one together from the runs that its tile lies in (the fewer tiles, the more runs each), every
+        // lane some of them with an activation's bytes in turn, then the lanes among themselves; and the CTAs of a cluster take turns
+        // with the sums over their ranks, which the others write to them (after the last barrier nobody touches another's memory).  The order is the same every time.
+        const int outs = nt_round * kTileN * rows, share = lanes_of_output(nt_round, outs);
+        float *own = reinterpret_cast<float *>(smem + prm.out_off);
+        auto store = [&](int o, float v) {
+            const int c = o & 15, q = o >> 4, tl = tile_of(q), m = q - tl * rows, n = (t0 + tl) * kTileN + c;
+            if (n >= prm.N) return;
+            v += !prm.bias ? 0.0f : t0 == t_first && o == out0 ? bias0 : __ldg(prm.bias + n);
             const int64_t at = (m0 + m) * prm.ldy + n;
             if (prm.y_f32) static_cast<float *>(prm.Y)[at] = v;
             else static_cast<__nv_bfloat16 *>(prm.Y)[at] = __float2bfloat16_rn(v);
+        };
+        for (int i = tid; i - lane < outs << share; i += kWarps * 32) {
+            const int o = i >> share, j = i & ((1 << share) - 1);
+            float v = 0.0f;
+            if (o < outs && total > 0) {
+                const int c = o & 15, q = o >> 4, tl = tile_of(q), m = q - tl * rows;
+                // the runs that units tl U .. tl U + U - 1 lie in
+                const int w_first = ((tl * U + 1) * kWarps - 1) / total, w_last = ((tl * U + U) * kWarps - 1) / total;
+                for (int w = w_first + j; w <= w_last; w += 1 << share) {
+                    if (w * total / kWarps == (w + 1) * total / kWarps) continue;     // a run of nothing (fewer units than warps)
+                    const float *from = (w == w_first ? red + tl * (prm.cols * kRedPitch) : head + w * (prm.cols * kRedPitch)) + m * kRedPitch + c;
+                    v += from[0] + from[prm.rows * kRedPitch] + from[2 * prm.rows * kRedPitch];
+                }
+            }
+            for (int d = 1; d < 1 << share; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+            if (o < outs && j == 0) {
+                if (cl > 1) {                            // to the CTA whose turn it is: [output / cl][rank]
+                    uint32_t at;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(own + (o & ~(cl - 1)) + rank)), "r"(o & (cl - 1)));
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+                } else {
+                    store(o, v);
+                }
+            }
         }
-        if (cl > 1) cluster_barrier();                   // nobody leaves, or writes new sums, while others read these
-        else if (t0 + prm.tiles_round < t_last) __syncthreads();
+        if (cl > 1) {
+            cluster_barrier();
+            for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
+                float v = 0.0f;
+                for (int r = 0; r < cl; r++) v += own[o - rank + r];
+                store(o, v);
+            }
+        }
+        if (t0 + prm.tiles_round < t_last) {             // the next tiles' sums take the place of these
+            if (cl > 1) cluster_barrier();
+            else __syncthreads();
+        }
     }
 }
 
@@ -835,21 +867,22 @@ bool lay_out(MatvecParams &p, int gb, int tiles)
     p.stage_bytes = (p.z_off + z_bytes + 127u) & ~127u;
     const size_t x_bytes = size_t(p.units_cta) * 4 * p.cols * 64, f_bytes = size_t(p.units_cta) * p.cols8 * 4,
                  xs_bytes = p.z ? gb * f_bytes : 0;
-    const size_t sum = size_t(p.cols) * kRedPitch * 4;
+    const size_t sum = size_t(p.cols) * kRedPitch * 4, one = sum + (p.cl > 1 ? size_t(p.rows) * kTileN * 4 : 0);      // of a tile
     for (p.stages = kMaxStages; p.stages >= 2; p.stages--) {
         const size_t fixed = size_t(kWarps * p.stages) * p.stage_bytes + x_bytes + f_bytes + xs_bytes + kWarps * sum;
-        if (fixed + std::min(tiles, 4) * sum > kMaxSmem) continue;
+        if (fixed + std::min(tiles, 4) * one > kMaxSmem) continue;
         p.x_off = uint32_t(kWarps * p.stages) * p.stage_bytes;
         p.f_off = uint32_t(p.x_off + x_bytes);
         p.xs_off = uint32_t(p.f_off + f_bytes);
         p.head_off = uint32_t(p.xs_off + xs_bytes);
         p.red_off = uint32_t(p.head_off + kWarps * sum);
-        p.tiles_round = int(std::min<size_t>(tiles, (kMaxSmem - fixed) / sum));
+        p.tiles_round = int(std::min<size_t>(tiles, (kMaxSmem - fixed) / one));
+        p.out_off = uint32_t(p.red_off + p.tiles_round * sum);
         return true;
     }
     return false;
 }
-size_t smem_bytes(const MatvecParams &p) { return p.red_off + size_t(p.tiles_round) * p.cols * kRedPitch * 4; }
+size_t smem_bytes(const MatvecParams &p) { return p.out_off + (p.cl > 1 ? size_t(p.tiles_round) * p.rows * kTileN * 4 : 0); }
 
 }  // namespace
 
@@ -891,7 +924,15 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
             p.clusters = std::min(p.tiles, dev.clusters[ci]);
             const int tiles = (p.tiles + p.clusters - 1) / p.clusters;
             if (!lay_out(p, gb, tiles)) continue;
-            const double cost = 0.055 * tiles * p.units_cta + (ci ? 0.6 : 0.0) + 0.003 * p.rows * p.units_cta;
+            // Microseconds, fitted to cl = 1, 2 and 4 forced on 16 shapes: a CTA's units (more columns and shorter groups take
+            // more instructions, a shallow ring waits more), converting its activations, its outputs, a cluster's
+            // barriers, and starting over where the tiles' sums do not fit at once.
+            const int nt = p.cols8 / 8;
+            const double unit = 0.035 + 0.02 * nt + (gb == 8 ? 0.02 : gb == 4 ? 0.007 : 0.0) * nt;
+            const double cost = unit * (1.0 + 0.1 * (kMaxStages - p.stages)) * tiles * p.units_cta +
+                                (p.act != SQ_ACT_NONE ? 0.05 : 0.035) * p.rows * p.units_cta +
+                                0.4 * ((tiles * kTileN * p.rows + kWarps * 32 - 1) / (kWarps * 32)) + (ci ? 0.9 : 0.0) +
+                                8.0 * ((tiles + p.tiles_round - 1) / p.tiles_round - 1);
             if (best == 0 || cost < best) best = cost, pick = p;
         }
         if (best != 0) break;
