@@ -324,6 +324,7 @@ struct MatvecParams {
     const void *X;
     int64_t ldx;
     int M, rows;                     // rows of X, rows of one pass (grid.y)
+    uint32_t per_row;                // 2^32 / rows, rounded up
     int K;
     int x_f32, x_wide, act;
     const uint8_t *W4;
@@ -419,6 +420,12 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Output o of a CTA's tiles is channel o % 16 of row o / 16 % rows; its tile, by a product (x / rows is the upper half of x times
+// per_row for x < 2^28 and rows > 1)
+__device__ __forceinline__ int tile_of_output(const MatvecParams &prm, int o)
+{
+    return prm.rows == 1 ? o >> 4 : int(__umulhi(uint32_t(o >> 4), prm.per_row));
+}
 // log2 of the lanes that put an output together: a tile lies in about 16 / tiles runs, and all threads together go through the
 // outputs once
 __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
@@ -509,13 +516,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
     };
     fetch();
     // the bias of this thread's first output, as far as that can be told before the tiles are split
-    const int tiles0 = min(prm.tiles_round, t_last - t_first);
-    const int out0 = cl > 1 ? tid * cl + rank : tid >> lanes_of_output(tiles0, tiles0 * kTileN * rows);
     float bias0 = 0.0f;
-    const uint32_t per_row = 0xFFFFFFFFu / uint32_t(rows) + 1u;      // x / rows = the upper half of x times this, for x < 2^28 and rows > 1
-    auto tile_of = [&](int q) { return rows == 1 ? q : int(__umulhi(uint32_t(q), per_row)); };
     if (prm.bias) {
-        const int n = (t_first + tile_of(out0 >> 4)) * kTileN + (out0 & 15);
+        const int tiles = min(prm.tiles_round, t_last - t_first);
+        const int o = cl > 1 ? tid * cl + rank : tid >> lanes_of_output(tiles, tiles * kTileN * prm.rows);
+        const int n = (t_first + tile_of_output(prm, o)) * kTileN + (o & 15);
         if (n < prm.N) bias0 = __ldg(prm.bias + n);
     }
 
@@ -746,12 +751,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         // ---- outputs.  2^share lanes put one together from the runs that its tile lies in (the fewer tiles, the more runs each), every
         // lane some of them with an activation's bytes in turn, then the lanes among themselves; and the CTAs of a cluster take turns
         // with the sums over their ranks, which the others write to them (after the last barrier nobody touches another's memory).  The order is the same every time.
-        const int outs = nt_round * kTileN * rows, share = lanes_of_output(nt_round, outs);
+        const int outs = nt_round * kTileN * prm.rows, share = lanes_of_output(nt_round, outs);       // (with those of rows behind the last)
         float *own = reinterpret_cast<float *>(smem + prm.out_off);
-        auto store = [&](int o, float v) {
-            const int c = o & 15, q = o >> 4, tl = tile_of(q), m = q - tl * rows, n = (t0 + tl) * kTileN + c;
-            if (n >= prm.N) return;
-            v += !prm.bias ? 0.0f : t0 == t_first && o == out0 ? bias0 : __ldg(prm.bias + n);
+        auto store = [&](int o, float v, bool first) {
+            const int c = o & 15, tl = tile_of_output(prm, o), m = (o >> 4) - tl * prm.rows, n = (t0 + tl) * kTileN + c;
+            if (n >= prm.N || m >= rows) return;
+            v += !prm.bias ? 0.0f : t0 == t_first && first ? bias0 : __ldg(prm.bias + n);
             const int64_t at = (m0 + m) * prm.ldy + n;
             if (prm.y_f32) static_cast<float *>(prm.Y)[at] = v;
             else static_cast<__nv_bfloat16 *>(prm.Y)[at] = __float2bfloat16_rn(v);
@@ -760,7 +765,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             const int o = i >> share, j = i & ((1 << share) - 1);
             float v = 0.0f;
             if (o < outs && total > 0) {
-                const int c = o & 15, q = o >> 4, tl = tile_of(q), m = q - tl * rows;
+                const int c = o & 15, tl = tile_of_output(prm, o), m = (o >> 4) - tl * prm.rows;
                 // the runs that units tl U .. tl U + U - 1 lie in
                 const int w_first = ((tl * U + 1) * kWarps - 1) / total, w_last = ((tl * U + U) * kWarps - 1) / total;
                 for (int w = w_first + j; w <= w_last; w += 1 << share) {
@@ -776,7 +781,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(own + (o & ~(cl - 1)) + rank)), "r"(o & (cl - 1)));
                     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
                 } else {
-                    store(o, v);
+                    store(o, v, i == tid);
                 }
             }
         }
@@ -785,7 +790,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             for (int o = tid * cl + rank; o < outs; o += kWarps * 32 * cl) {
                 float v = 0.0f;
                 for (int r = 0; r < cl; r++) v += own[o - rank + r];
-                store(o, v);
+                store(o, v, o == tid * cl + rank);
             }
         }
         if (t0 + prm.tiles_round < t_last) {             // the next tiles' sums take the place of these
@@ -916,6 +921,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     for (;; passes++) {
         p.rows = (p.M + passes - 1) / passes;
         p.cols = p.rows * 3;
+        p.per_row = 0xFFFFFFFFu / uint32_t(p.rows) + 1u;
         p.cols8 = (p.cols + 7) / 8 * 8;
         for (int ci = 0; ci < 4; ci++) {
             p.cl = 1 << ci;
