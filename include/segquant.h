@@ -314,7 +314,7 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     longer one) are exact, the rest is fp32 in an order that depends on the sizes and the device alone; one
  *     rounding to y_dtype.  A row with an infinity or a NaN among its activations has NaN for outputs.  X [M,K] dev (dtype dt, ldx
  *     elements), bias dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements
- *     only; Y must not overlap X.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072; any M, meant for M of at most about 32
+ *     only; Y must not overlap X, bias or Wq4.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072; any M, meant for M of at most about 32
  *     (the weights are read once per pass of up to 10 rows).  No workspace.
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
  *     N <= 4194240 for segquant_dequantize_w4_group. */

@@ -218,6 +218,16 @@ static sq_status check_block_norm(const BlockNormArgs &a)
         if (rows_overlap(c, a.ldc, a.C, a.H, out[0].pitch, bytes, a.M)) return SQ_ERR_UNSUPPORTED;
     }
     if (rows_overlap(a.c_pos, a.ldc, a.C, a.c_neg, a.ldc, a.C, a.M)) return SQ_ERR_UNSUPPORTED;
+    // nor may one take a vector's place, which all rows read
+    const int64_t samples = (a.M - 1) / n->rows_per_sample + 1, ps = int64_t(dt_size(n->p_dtype));
+    const struct { const void *p; int64_t ld; } vectors[7] = {{n->post_w, 0}, {n->post_b, 0}, {n->w, 0}, {n->b, 0}, {n->gate, n->ld_gate},
+                                                              {n->scale, n->ld_scale}, {n->shift, n->ld_shift}};
+    const struct { const void *p; int64_t pitch, width; } written[4] = {{a.H, out[0].pitch, bytes}, {a.O, out[1].pitch, bytes},
+                                                                        {a.c_pos, a.ldc, a.C}, {a.c_neg, a.ldc, a.C}};
+    for (const auto &v : vectors)
+        for (const auto &o : written)
+            if (v.p && o.p && overlap(v.p, size_t(((samples - 1) * v.ld + a.C) * ps), o.p, size_t((a.M - 1) * o.pitch + o.width)))
+                return SQ_ERR_UNSUPPORTED;
     return SQ_OK;
 }
 
@@ -580,6 +590,7 @@ sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int6
     sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
     if (st != SQ_OK) return st;
     if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
+    if (overlap(W, size_t((N - 1) * ld + K) * dt_size(dt), Wq4, size_t((N - 1) * ldw + (K + 1) / 2))) return SQ_ERR_UNSUPPORTED;
     return launch_quantize_w4_group(W, dt, N, K, ld, group, Wq4, ldw, s_w, s_dtype, lds, z_w, ldz, static_cast<cudaStream_t>(stream));
 }
 
@@ -591,6 +602,7 @@ sq_status segquant_dequantize_w4_group(const void *Wq4, int64_t ldw, int64_t N, 
     sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
     if (st != SQ_OK) return st;
     if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
+    if (overlap(W, size_t((N - 1) * ld + K) * dt_size(dt), Wq4, size_t((N - 1) * ldw + (K + 1) / 2))) return SQ_ERR_UNSUPPORTED;
     return launch_dequantize_w4_group(Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz, W, dt, ld, static_cast<cudaStream_t>(stream));
 }
 
@@ -607,7 +619,9 @@ sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, i
     const int64_t xs = int64_t(dt_size(dt)), ys = int64_t(dt_size(y_dtype));
     if (reinterpret_cast<uintptr_t>(X) % xs || reinterpret_cast<uintptr_t>(Y) % ys || (reinterpret_cast<uintptr_t>(bias) & 3u))
         return SQ_ERR_ALIGN;
-    if (rows_overlap(X, ldx * xs, K * xs, Y, ldy * ys, N * ys, M)) return SQ_ERR_UNSUPPORTED;
+    const size_t y_bytes = size_t((M - 1) * ldy + N) * ys;
+    if (rows_overlap(X, ldx * xs, K * xs, Y, ldy * ys, N * ys, M) || (bias && overlap(bias, size_t(N) * 4, Y, y_bytes))) return SQ_ERR_UNSUPPORTED;
+    if (overlap(Wq4, size_t((N - 1) * ldw + (K + 1) / 2), Y, y_bytes)) return SQ_ERR_UNSUPPORTED;
     return launch_w4_matvec({X, dt, M, K, ldx, act, Wq4, ldw, N, group, s_w, s_dtype, lds, z_w, ldz, bias, Y, y_dtype, ldy},
                             static_cast<cudaStream_t>(stream));
 }

@@ -17,16 +17,11 @@
 // instructions, which waited for its own code (8858 x 1536 bf16, two RMS norms: 63.6 us; gated and modulated to codes 135 us).
 #include <cuda_bf16.h>
 #include <algorithm>
-#include <atomic>
-#include <mutex>
-#include <vector>
 #include "quant_codes.cuh"
 
 namespace sq {
 
 enum : int { kOutValues = 0, kOutInt8 = 1, kOutInt8Dual = 2, kOutE4m3 = 3, kOutE4m3Dual = 4 };
-
-constexpr int kMaxVectorBytes = 220 * 1024;       // of the vectors in shared memory
 
 struct BlockNormParams {
     const void *Y, *R;
@@ -57,6 +52,8 @@ struct BlockNormParams {
 
 #ifdef SQ_NORM_OUT     // the kernels of one kind of output; the kinds are compiled side by side
 namespace {
+
+constexpr int kMaxVectorBytes = 220 * 1024;       // of the vectors in shared memory
 
 template <typename T> struct Chunk;                     // eight elements as loaded
 template <> struct Chunk<float> { uint4 v[2]; };
@@ -487,8 +484,9 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
 }
 
 // One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1280 bf16 (1024 fp32) channels
-// where there are rows enough for that, two and four up to 4096, then a block per row; few rows get a block each, and so do rows that have
-// vectors of their own.  (8858 x 1536 bf16 to codes: one warp with six chunks a lane, held to 128 registers, 28.1 us; two with three
+// where there are at least five per SM, two and four up to 4096, then a block per row; fewer rows get a block each.  Rows of up to 128
+// channels take 8 or 16 lanes (32768 x 64: 14.1 -> 5.5 us).  Samples of fewer than 16 rows: every row makes its vectors (16384 x 640, a vector
+// per row: 93.7 us with a block per row, 51.4 with a warp).  (8858 x 1536 bf16 to codes: one warp with six chunks a lane, held to 128 registers, 28.1 us; two with three
 // 23.1 us.  32768 x 1280: one warp with five chunks 55.8 us, two with three, of which one sixth is idle, 63.2 us.)
 template <typename T, int OUT>
 sq_status run_shape(BlockNormParams p, cudaStream_t st)

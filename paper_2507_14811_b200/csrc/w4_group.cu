@@ -4,10 +4,10 @@
 //   w'[n][k] = (c[n][k] - z[g][n]) s[g][n],  g = k / group          y[m][n] = sum_g s[g][n] sum_{k in g} (c - z) a(x[m][k]) + b[n]
 //
 // The product is bound by reading the codes once: N K / 2 bytes, 12.8 T codes a second at copy bandwidth.  That leaves 148 SMs 2.8 lane
-// instructions per code, and half of that on either arithmetic pipe, so codes are not turned into real numbers one by one.  A byte of two
-// codes is two signed bytes 16 c after one mask each (0.4 instructions per code), which integer matrix instructions take as they are:
-// mma.m16n8k32, 16 channels on its rows.  The activations become 23-bit fixed-point numbers of their group's range, as three signed
-// bytes in three of its 8 columns; products and a group's sums are exact integers, and scales and zero-points come in behind a group.
+// instructions per code, and half of that on either arithmetic pipe, so codes are not turned into real numbers one by one.  A byte of
+// two codes is two signed bytes 16 c after one mask each (0.4 instructions per code), which integer matrix instructions take as they are:
+// mma.m16n8k32, 16 channels on its rows.  The activations become 23-bit fixed-point numbers, as three signed bytes in three of
+// its 8 columns; products and a group's sums are exact integers, and scales and zero-points come in behind a group.
 // (Expanded to bf16 instead, 1.4 instructions per code, the same design took 38.3 us for 1 x 8192 -> 28672 with zero-points.)  tcgen05
 // would want the expanded codes in shared memory, twice the bytes that came in, and has nothing to offer: the tensor pipe is no bound here.
 #include <cuda_bf16.h>
@@ -121,7 +121,8 @@ __device__ __noinline__ uint2 codes16_slow(const float *x, float s, float lo, fl
 // out first; LANES lanes of a group agree on its extrema by shuffles, and the codes leave as 256 consecutive bytes.  Groups longer
 // than 512 (LONG) read the channel's group twice, the second time from cache.  Scales and zero-points are [groups][N]; a block
 // gathers those of its channels in shared memory, so that they leave as runs.  (Eight inputs per lane and loops for any group: 43
-// instructions per weight, 128 us for 18432 x 4608 bf16; 16 inputs and fixed lanes 64 us with two channels, XX with four.)
+// instructions per weight, 128 us for 18432 x 4608 bf16; 16 inputs and fixed lanes, 16 instructions, 64 us, with two channels per warp as with four: what is left is
+// a warp's chain of shuffles, divisions and conversions at 24 to 32 warps per SM.)
 template <typename Tin, bool ZP, int LANES, bool LONG>
 __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_constant__ W4QuantParams prm)
 {
@@ -439,7 +440,7 @@ __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
 // tile after tile of 16 channels, and every warp takes an equal run of that list: whole tiles, and the end of one and the start of
 // another.  So no warp waits for another until all of them are done, whatever the number of channels and inputs (one tile at a time, K shared by
 // the warps and their sums joined behind each, took half as long again).  A tile's sum is then put together from the runs that it lies
-// in, in their order.  K may also be shared by the `cl` CTAs of a cluster, which read one another's sums.
+// in, in their order.  K may also be shared by the `cl` CTAs of a cluster, which write their sums to one another.
 // Every warp streams its units through a ring of its own (asynchronous copies; nothing but the warp itself waits for them).
 //
 // Codes of one channel that share 16 bytes are handed to the four lanes of a row by ldmatrix, eight each: (w << 4) & 0xF0F0F0F0 are the
@@ -452,7 +453,7 @@ __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
 // zero-points in [-8, 7], so that it becomes a float by starting at the bits of 1.5 * 2^23 and subtracting that number: the start,
 // less the zero-point times the block's sum of q_i, is the MMA's addend.  One FMA in fp32 takes it with its scale to the unit's sum, and one
 // the unit's sum with 2^(E - 25) 256^i to the tile's.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
-// instead: 27.6 us for 1 x 8192 -> 28672, where one per unit takes XX; 10.0 us for 8 x 1536 -> 9216 with SiLU instead of YY.)
+// instead of one per unit: 26.3 us against 25.8 for 1 x 8192 -> 28672, 9.7 against 8.8 for 8 x 1536 -> 9216 with SiLU.)
 // GB: blocks of a unit (2, 4, 8).
 template <int NT, int GB, bool ZP>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_constant__ MatvecParams prm)

@@ -38,10 +38,11 @@ def test_group_quantizer_refusals(L, back):
     assert q(W=FAKE + 4) == 4 and q(ld=258) == 4 and q(W4=FAKE + 8) == 4 and q(ldw=136) == 4 and q(s=FAKE + 4) == 4 and q(lds=66) == 4
     assert q(sdt=1, lds=68) == 4 and q(z=FAKE + 8) == 4 and q(z=FAKE, ldz=72) == 4
     assert q(dt=5) == 5 and q(sdt=5) == 5
+    assert q(W4=FAKE + 1024) == 5                               # codes in the weights' memory
     for group in (0, -32, 16, 48, 96, 192, 255, 300):
         assert q(group=group) == 5, group
     if back:
-        assert q(N=1 << 23, lds=1 << 23) == 2                   # more channel blocks than a grid has
+        assert q(N=1 << 23, lds=1 << 23, W=1 << 44) == 2                   # more channel blocks than a grid has
 
 
 def matvec(L, X=FAKE, dt=1, M=4, K=256, ldx=256, act=0, W4=2 * FAKE, ldw=128, N=64, group=64, s=3 * FAKE, sdt=0, lds=64, z=0, ldz=64,
@@ -59,6 +60,7 @@ def test_matvec_refusals(L):
     assert m(X=FAKE + 1) == 4 and m(Y=FAKE + 1) == 4 and m(ydt=0, Y=4 * FAKE + 2) == 4 and m(bias=FAKE + 2) == 4 and m(W4=2 * FAKE + 8) == 4
     assert m(dt=2) == 5 and m(ydt=2) == 5 and m(act=3) == 5 and m(act=9) == 5 and m(group=100) == 5
     assert m(Y=FAKE) == 5 and m(Y=FAKE + 4 * 512 - 2) == 5      # Y in X's memory
+    assert m(bias=4 * FAKE + 256) == 5 and m(Y=2 * FAKE + 64 * 128 - 2) == 5           # .. the bias's, the weights'
 
 
 class Norm(C.Structure):
@@ -92,6 +94,7 @@ def test_block_norm_refusals(L, codes):
     assert b(dt=3) == 5 and b(p_dtype=3) == 5 and b(pre=3) == 5 and b(Y=2 * FAKE, post=7) == 5 and b(eps=-1.0) == 5 and b(eps=float("nan")) == 5
     assert b(H=FAKE + 256) == 5                                               # the new stream one row off the old one
     assert b(Y=2 * FAKE, H=2 * FAKE + 256) == 5
+    assert b(H=3 * FAKE, w=3 * FAKE + 256) == 5 and b(H=3 * FAKE, scale=3 * FAKE - 400, ld_scale=64, rows_per_sample=2) == 5    # a vector's place
     if codes:
         assert b(s_pos=0) == 1 and b(c_pos=0) == 1 and b(s_neg=FAKE, c_neg=0) == 1
         assert b(ldc=48) == 2 and b(seg=B.SegTable([0, 32], [0, 8])) == 3 and b(ldc=72) == 4 and b(code=4) == 5
