@@ -398,3 +398,56 @@ def test_refusals_on_the_gpu():
     with pytest.raises(B.SegquantError, match="UNSUPPORTED"):
         B.segquant_block_norm(both[:8], out=both[1:])         # a row further on: overwritten before it is read
     B.segquant_block_norm(torch.zeros((4, 128), device=DEV)[:, :64], out=torch.zeros((4, 128), device=DEV)[:, 64:])
+
+
+def test_a_captured_block():
+    """Modulation, norm and layer in one graph, replayed on new inputs: the bits of the eager calls.  The kernels start before the
+    ones in front of them are done; each must wait for what it reads."""
+    g = torch.Generator().manual_seed(6)
+    samples, T, C = 2, 700, 384
+    mod = W4GroupLinear(torch.randn((3 * C, C), generator=g) * 0.03, torch.randn(3 * C, generator=g) * 0.1, group=128, zero_points=True)
+    fc = SegQuantLinear(torch.randn((512, C), generator=g) * 0.05, torch.randn(512, generator=g) * 0.1, [0, C], [0, 512], True)
+    new = lambda: (torch.randn((samples, C), generator=g).to(DEV), torch.randn((samples * T, C), generator=g).to(DEV).to(BF),
+                   torch.randn((samples * T, C), generator=g).to(DEV).to(BF))
+    fc.calibrate(torch.randn((64, C), generator=g).to(BF))
+
+    def block(c, R, X):
+        shift, scale, gate = mod.forward(c, act="silu").chunk(3, 1)
+        return fc.forward_block(R, X, gate=gate, scale=scale, shift=shift, rows_per_sample=T)
+
+    static = [t.clone() for t in new()]
+    block(*static)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        H, Y = block(*static)
+    for _ in range(3):
+        fresh = new()
+        for s, f in zip(static, fresh):
+            s.copy_(f)
+        graph.replay()
+        want = block(*fresh)
+        torch.cuda.synchronize()
+        assert torch.equal(H, want[0]) and torch.equal(Y, want[1])
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """What is looked up once per device and kernel is looked up outside of the stream."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2507_14811_b200 import binding as B
+X, W4 = torch.ones((1, 4096), device="cuda", dtype=torch.bfloat16), torch.full((64, 2048), 0x11, dtype=torch.uint8, device="cuda")
+s, R = torch.ones((32, 64), device="cuda"), torch.ones((1200, 4096), device="cuda")
+v = torch.ones(4096, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    Y = B.segquant_w4_matvec(X, W4, s, 128, y_dtype=torch.float32)
+    H, O = B.segquant_block_norm(R, R, gate=v, norm="rms", eps=0.0, w=v, b=v)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.all(Y == 4096) and torch.all(H == 2) and torch.all(O == 2)
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=300)
