@@ -240,70 +240,90 @@ struct W4DequantParams {
     int64_t groups;
 };
 
-// The reverse, bound by writing W: a lane turns four bytes into eight values; the block's scales come through shared memory.
+// Eight codes -> eight values in order.  A nibble with its top bit flipped is c + 8, and the bits 0x4300 | (c + 8) are the bf16 number
+// 136 + c: codes i and i + 4 of a word in one shift and one mask.  neg_off: -(136 + z), twice; the product is the one fp32 product.
+__device__ __forceinline__ void values8(uint32_t word, uint64_t neg_off, uint64_t s2, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t pair = (word >> (4 * i) & 0x000F000Fu) ^ 0x43084308u;
+        unpack2(mul2(add2(pack2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u)), neg_off), s2), v[i], v[i + 4]);
+    }
+}
+template <typename Tout>
+__device__ __forceinline__ void store8(Tout *out, const float (&v)[8])
+{
+    if (sizeof(Tout) == 4) {
+        reinterpret_cast<float4 *>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        __nv_bfloat162 b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) b[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(b);
+    }
+}
+
+// The reverse, bound by writing W: a lane turns four bytes into eight values, for eight channels whose words it has loaded first; the block's
+// scales and zero-points come through shared memory.  (One code at a time and bounds for every word: 14.5 instructions per weight, 49 us for
+// 18432 x 4608 in groups of 32 with zero-points, 76 % of the issue slots; now 47, and 36 instead of 42 in groups of 128.)
 template <typename Tout>
 __global__ void __launch_bounds__(256) dequantize_w4_group_kernel(const __grid_constant__ W4DequantParams prm)
 {
-    __shared__ float sm_s[8][kTileRows];
-    __shared__ float sm_z[8][kTileRows];
+    __shared__ float sm_s[8][kTileRows + 1];             // (a pitch that keeps the groups of a channel on different banks)
+    __shared__ float sm_z[8][kTileRows + 1];             // -(136 + z)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n0 = int64_t(blockIdx.y) * kTileRows, k0 = int64_t(blockIdx.x) * kTileK, g0 = k0 / prm.group;
     const int in_block = prm.group >= kTileK ? 1 : kTileK / prm.group;
+    const bool inside = n0 + kTileRows <= prm.N && k0 + kTileK <= prm.K;
     uint32_t word[kRowsPerWarp];
-    const int64_t k = k0 + lane * 8;
+    const int64_t k = k0 + lane * 8, n = n0 + warp * kRowsPerWarp;
+    const uint8_t *p = prm.W4 + n * prm.ldw + k / 2;
+    if (inside) {
 #pragma unroll
-    for (int r = 0; r < kRowsPerWarp; r++) {
-        const int64_t n = n0 + warp * kRowsPerWarp + r;
-        word[r] = 0;
-        if (n < prm.N && k < prm.K) {
-            const uint8_t *p = prm.W4 + n * prm.ldw + k / 2;
-            if (k + 8 <= prm.K) {
-                word[r] = __ldg(reinterpret_cast<const uint32_t *>(p));
-            } else {
-                for (int j = 0; k + 2 * j < prm.K; j++) word[r] |= uint32_t(__ldg(p + j)) << (8 * j);
+        for (int r = 0; r < kRowsPerWarp; r++) word[r] = __ldg(reinterpret_cast<const uint32_t *>(p + r * prm.ldw));
+    } else {
+#pragma unroll
+        for (int r = 0; r < kRowsPerWarp; r++) {
+            word[r] = 0;
+            if (n + r < prm.N && k < prm.K) {
+                if (k + 8 <= prm.K) word[r] = __ldg(reinterpret_cast<const uint32_t *>(p + r * prm.ldw));
+                else for (int j = 0; k + 2 * j < prm.K; j++) word[r] |= uint32_t(__ldg(p + r * prm.ldw + j)) << (8 * j);
             }
         }
     }
     for (int i = threadIdx.x; i < in_block * kTileRows; i += blockDim.x) {
-        const int64_t g = g0 + i / kTileRows, n = n0 + i % kTileRows;
+        const int64_t g = g0 + i / kTileRows, m = n0 + i % kTileRows;
         float s = 0.0f, z = 0.0f;
-        if (g < prm.groups && n < prm.N) {
-            s = prm.s_bf16 ? load1(static_cast<const __nv_bfloat16 *>(prm.s) + g * prm.lds + n)
-                           : __ldg(static_cast<const float *>(prm.s) + g * prm.lds + n);
-            if (prm.z) z = float(prm.z[g * prm.ldz + n]);
+        if (g < prm.groups && m < prm.N) {
+            s = prm.s_bf16 ? load1(static_cast<const __nv_bfloat16 *>(prm.s) + g * prm.lds + m)
+                           : __ldg(static_cast<const float *>(prm.s) + g * prm.lds + m);
+            if (prm.z) z = float(prm.z[g * prm.ldz + m]);
         }
         sm_s[i / kTileRows][i % kTileRows] = s;
-        sm_z[i / kTileRows][i % kTileRows] = z;
+        sm_z[i / kTileRows][i % kTileRows] = -136.0f - z;
     }
     __syncthreads();
     if (k >= prm.K) return;
     const int gi = prm.group >= kTileK ? 0 : lane * 8 / prm.group;
+    Tout *out = static_cast<Tout *>(prm.W) + n * prm.ld + k;
 #pragma unroll
     for (int r = 0; r < kRowsPerWarp; r++) {
-        const int64_t n = n0 + warp * kRowsPerWarp + r;
-        if (n >= prm.N) return;
-        // a nibble with its top bit flipped is c + 8; below the bits of 2^23 it makes the float 2^23 + 8 + c
-        const float s = sm_s[gi][warp * kRowsPerWarp + r], z = sm_z[gi][warp * kRowsPerWarp + r] + 8388616.0f;
+        const float s = sm_s[gi][warp * kRowsPerWarp + r], z = sm_z[gi][warp * kRowsPerWarp + r];
         float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = __fmul_rn(__uint_as_float((word[r] >> (4 * i) & 15u) ^ 0x4B000008u) - z, s);
-        Tout *out = static_cast<Tout *>(prm.W) + n * prm.ld + k;
-        if (k + 8 <= prm.K) {
-            if (sizeof(Tout) == 4) {
-                reinterpret_cast<float4 *>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4 *>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        values8(word[r], pack2(z, z), pack2(s, s), v);
+        if (inside) {
+            store8(out + r * prm.ld, v);
+        } else if (n + r < prm.N) {
+            if (k + 8 <= prm.K) {
+                store8(out + r * prm.ld, v);
             } else {
-                __nv_bfloat162 b[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) b[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(b);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (k + i >= prm.K) break;
-                if (sizeof(Tout) == 4) reinterpret_cast<float *>(out)[i] = v[i];
-                else reinterpret_cast<__nv_bfloat16 *>(out)[i] = __float2bfloat16_rn(v[i]);
+                for (int i = 0; i < 8; i++) {
+                    if (k + i >= prm.K) break;
+                    if (sizeof(Tout) == 4) reinterpret_cast<float *>(out + r * prm.ld)[i] = v[i];
+                    else reinterpret_cast<__nv_bfloat16 *>(out + r * prm.ld)[i] = __float2bfloat16_rn(v[i]);
+                }
             }
         }
     }
