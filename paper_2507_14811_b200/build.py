@@ -62,7 +62,7 @@ def build_calls(nvcc: str) -> None:
         os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f for d in include for f in ("-isystem", d)],
         "-I", INCLUDE, os.path.join(CSRC, "torch_calls.cpp"), "-o", CALLS_PATH, "-L", _HERE, "-l:libsegquant.so",
-        *[f for d in cpp_extension.library_paths() for f in ("-L", d)], "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+        *[f for d in cpp_extension.library_paths() for f in ("-L", d)], "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
         "-Wl,-rpath,$ORIGIN"])
 
 
