@@ -63,6 +63,26 @@ __device__ __forceinline__ void load32(const void *p, uint4 &a, uint4 &b)
         : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
 }
 
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// x / d, correctly rounded, for d = 7 or 15 and r = RN(1 / d): a quotient corrected by its remainder (checked on the CPU for all
+// significands against the IEEE division), for x that its remainder does not underflow for
+__device__ __forceinline__ float over(float x, float d, float r)
+{
+    const float q = x * r;
+    return fmaf(fmaf(-q, d, x), r, q);
+}
+
 struct W4QuantParams {
     const void *W;
     int64_t ld;
@@ -121,8 +141,8 @@ __device__ __noinline__ uint2 codes16_slow(const float *x, float s, float lo, fl
 // out first; LANES lanes of a group agree on its extrema by shuffles, and the codes leave as 256 consecutive bytes.  Groups longer
 // than 512 (LONG) read the channel's group twice, the second time from cache.  Scales and zero-points are [groups][N]; a block
 // gathers those of its channels in shared memory, so that they leave as runs.  (Eight inputs per lane and loops for any group: 43
-// instructions per weight, 128 us for 18432 x 4608 bf16; 16 inputs and fixed lanes, 16 instructions, 64 us, with two channels per warp as with four: what is left is
-// a warp's chain of shuffles, divisions and conversions at 24 to 32 warps per SM.)
+// instructions per weight, 128 us for 18432 x 4608 bf16; 16 inputs and fixed lanes, 16 instructions, 64 us, with two channels per warp
+// as with four and at 24 as at 32 warps, as long as a row's branches kept the rows one behind the other; without them 41 us.)
 template <typename Tin, bool ZP, int LANES, bool LONG>
 __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_constant__ W4QuantParams prm)
 {
@@ -147,6 +167,76 @@ __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_con
                 else raw[r][i] = __ldg(p), raw[r][i + 1] = __ldg(p + 1);
             }
     }
+    // The usual case in one go, without a branch for the rows to wait at: ranges and scales inside the fast form.
+    bool done = false;
+    if (!LONG && inside) {
+        auto expand = [&](int r, float (&x)[16]) {
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(raw[r]);
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                x[i] = sizeof(Tin) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        };
+        float hi[ROWS], neg[ROWS], s[ROWS], z[ROWS];
+        SegConst c[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; r++) {
+            if (sizeof(Tin) == 2) {                      // two at a time
+                const uint32_t *w = reinterpret_cast<const uint32_t *>(raw[r]);
+                uint32_t top = w[0], low = w[0];
+#pragma unroll
+                for (int i = 1; i < 8; i++) top = max_bf16x2(top, w[i]), low = min_bf16x2(low, w[i]);
+                hi[r] = fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u));
+                neg[r] = -fminf(__uint_as_float(low << 16), __uint_as_float(low & 0xFFFF0000u));
+            } else {
+                float x[16];
+                expand(r, x);
+                hi[r] = x[0], neg[r] = -x[0];
+#pragma unroll
+                for (int i = 1; i < 16; i++) hi[r] = fmaxf(hi[r], x[i]), neg[r] = fmaxf(neg[r], -x[i]);
+            }
+            if (!ZP) hi[r] = fmaxf(hi[r], neg[r]);
+        }
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) {
+#pragma unroll
+            for (int r = 0; r < ROWS; r++) {
+                hi[r] = fmaxf(hi[r], __shfl_xor_sync(0xFFFFFFFFu, hi[r], o));
+                if (ZP) neg[r] = fmaxf(neg[r], __shfl_xor_sync(0xFFFFFFFFu, neg[r], o));
+            }
+        }
+        bool easy = true;
+#pragma unroll
+        for (int r = 0; r < ROWS; r++) {
+            hi[r] = fmaxf(hi[r], 0.0f), neg[r] = fmaxf(neg[r], 0.0f);
+            const float range = ZP ? __fadd_rn(hi[r], neg[r]) : hi[r];
+            s[r] = stored_scale(ZP ? over(range, 15.0f, 1.0f / 15.0f) : over(range, 7.0f, 1.0f / 7.0f), prm.s_bf16);
+            c[r] = seg_const(s[r]);
+            easy = easy && range >= 1e-25f && c[r].fast;
+            z[r] = 0.0f;                                 // (-8 - round(lo / s): rounding is symmetric; the quotient as the codes')
+            if (ZP) {
+                const float q = neg[r] * c[r].r;
+                z[r] = (fmaf(fmaf(-q, s[r], neg[r]), c[r].r, q) + kRoundMagic - kRoundMagic) - 8.0f;
+            }
+        }
+        done = __all_sync(0xFFFFFFFFu, easy);
+        if (done) {
+            uint8_t *out = prm.W4 + n0 * prm.ldw + k0 / 2;
+#pragma unroll
+            for (int r = 0; r < ROWS; r++) {
+                float x[16];
+                expand(r, x);
+                const uint32_t z4 = (__float_as_uint(z[r] + kRoundMagic) & 15u) * 0x01010101u;
+                *reinterpret_cast<uint2 *>(out + r * prm.ldw) = codes16<ZP>(x, c[r], 7.0f - z[r], z4);
+            }
+            if (lane % LANES == 0) {
+#pragma unroll
+                for (int r = 0; r < ROWS; r++) {
+                    sm_s[lane / LANES][warp * ROWS + r] = s[r];
+                    if (ZP) sm_z[lane / LANES][warp * ROWS + r] = int8_t(int(__float_as_uint(z[r] + kRoundMagic)) - kMagicBits);
+                }
+            }
+        }
+    }
     auto load16 = [&](int r, int k, float (&x)[16]) {
         float a[8], b[8];
         if (n0 + r < prm.N) {
@@ -159,17 +249,10 @@ __global__ void __launch_bounds__(256) quantize_w4_group_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < 8; i++) x[i] = a[i], x[i + 8] = b[i];
     };
-#pragma unroll
-    for (int r = 0; r < ROWS; r++) {
+#pragma unroll 1
+    for (int r = 0; r < ROWS && !done; r++) {
         float x[16];
-        if (inside) {
-            const uint32_t *w = reinterpret_cast<const uint32_t *>(raw[r]);
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-                x[i] = sizeof(Tin) == 4 ? __uint_as_float(w[i]) : __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-        } else {
-            load16(r, k0, x);
-        }
+        load16(r, k0, x);
         float hi = 0.0f, neg = 0.0f;                     // extrema: of both polarities (hi, -lo), or of the magnitude
         auto extrema = [&](const float (&v)[16]) {
 #pragma unroll
