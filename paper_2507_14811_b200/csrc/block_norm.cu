@@ -37,7 +37,7 @@ struct BlockNormParams {
     int vec;                          // bit i: vector i of post_w, post_b, w, b, gate, scale, shift may be read 16 bytes at a time
     int has;                          // bits: which of P, Q, A, B there are
     int sm_at[4];                     // where they lie in shared memory
-    int half;                         // floats of half a vector there
+    int pitch, half;                  // floats of a vector there (eight zeros at the end), of half a one
     int own;                          // floats of a row's own vectors there (0: rows share them)
     int two_steps;                    // shared memory holds P and Q or A and B
     float alpha, eps, inv_c;
@@ -114,23 +114,30 @@ __device__ __noinline__ void store_tail(T *p, int left, Eight x)
         }
 }
 template <typename T>
+__device__ __forceinline__ void store_whole(T *p, const uint64_t (&pairs)[4])
+{
+    float x[8];
+    singles(pairs, x);
+    if (sizeof(T) == 4) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <typename T>
 __device__ __forceinline__ void store_chunk(T *row, int col, int C, const uint64_t (&pairs)[4])
 {
     float x[8];
     singles(pairs, x);
     if (col + 8 <= C) {
-        if (sizeof(T) == 4) {
-            reinterpret_cast<float4 *>(row + col)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4 *>(row + col)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t *>(&b);
-            }
-            *reinterpret_cast<uint4 *>(row + col) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        store_whole(row + col, pairs);
     } else {
         Eight e;
 #pragma unroll
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
     // this block's rows, and its row group's first
     const int r0 = int(int64_t(blockIdx.x) * prm.M / gridDim.x), r1 = int((int64_t(blockIdx.x) + 1) * prm.M / gridDim.x);
     int m = r0 + row_of_block, sample = -1;
-    int col[CH];
+    int col[CH], at[CH];
     Chunk<T> y[CH], r[CH];
     auto fetch = [&](int row) {
 #pragma unroll
@@ -327,7 +334,11 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
         }
     };
 #pragma unroll
-    for (int c = 0; c < CH; c++) col[c] = ((c * WPR + warp_of_row) * L + lane) * 8;
+    for (int c = 0; c < CH; c++) {
+        col[c] = ((c * WPR + warp_of_row) * L + lane) * 8;
+        at[c] = col[c] < C ? col[c] : prm.pitch - 8;           // its vectors: behind the row's end zeros
+        if (!Y || !R) y[c] = r[c] = Chunk<T>{};
+    }
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");     // nothing is read before the kernel in front is done
     if (m < r1) fetch(m);
 
@@ -347,7 +358,19 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
             seg[c] = uint32_t(p) | (fast ? 0u : 0x80000000u);
         }
     }
+    bool all_fast = CODES;
+#pragma unroll
+    for (int c = 0; c < CH; c++) all_fast = all_fast && (col[c] >= C || !(seg[CODES ? c : 0] >> 31));
+    all_fast = __all_sync(0xFFFFFFFFu, all_fast);
     float *red = sm_red + (WPR > 1 ? row_of_block * 4 * WPR : 0);
+    // zeros behind every vector; with vectors of its own each row has them
+    if (lane < 8 && warp_of_row == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (prm.has >> i & 1) vec[prm.sm_at[i] + (lane < 4 ? 0 : prm.half) + prm.pitch / 2 - 4 + (lane & 3)] = 0.0f;
+    }
+    if (WPR > 1) __syncthreads();
+    else __syncwarp();
     for (int start = r0, end; start < r1; start = end) {
         end = r1;
         if (!OWN) {                                            // the rows of one sample
@@ -375,6 +398,8 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
                 }
             }
             if (OWN && RPB == 1 && prm.two_steps) sample = m / prm.rows_per_sample;
+            // Branches stand around loops over the chunks, not inside them, so that the chunks of a row are worked on side by side;
+            // chunks behind the row's end read zeros for its vectors and stay zero, and only stores ask where they are.
             uint64_t h[CH][4];
             if (Y) {
 #pragma unroll
@@ -393,21 +418,44 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
                         if (k < C) make_post(prm, vec, sample, k);
                     }
                 }
+                const float *vp = vec + prm.sm_at[kP], *vq = vec + prm.sm_at[kQ];
+                const int with = prm.has & (1 << kP | 1 << kQ);
+                if (with == (1 << kP | 1 << kQ)) {
 #pragma unroll
-                for (int c = 0; c < CH; c++) {
-                    if (col[c] >= C) continue;
-                    uint64_t v[4], x[4] = {0, 0, 0, 0};
-                    if (R) expand(r[c], x);
-                    if (prm.has >> kQ & 1) {
-                        get8(vec + prm.sm_at[kQ], prm.half, col[c], v);
+                    for (int c = 0; c < CH; c++) {
+                        uint64_t v[4], w[4], x[4];
+                        expand(r[c], x);
+                        get8(vp, prm.half, at[c], v);
+                        get8(vq, prm.half, at[c], w);
 #pragma unroll
-                        for (int i = 0; i < 4; i++) x[i] = add2(x[i], v[i]);
+                        for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], add2(x[i], w[i]));
                     }
-                    if (prm.has >> kP & 1) {
-                        get8(vec + prm.sm_at[kP], prm.half, col[c], v);
+                } else if (with) {
+                    const bool p_only = with == 1 << kP;
+                    if (p_only) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], x[i]);
+                        for (int c = 0; c < CH; c++) {
+                            uint64_t v[4], x[4];
+                            expand(r[c], x);
+                            get8(vp, prm.half, at[c], v);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], x[i]);
+                        }
                     } else {
+#pragma unroll
+                        for (int c = 0; c < CH; c++) {
+                            uint64_t v[4], x[4];
+                            expand(r[c], x);
+                            get8(vq, prm.half, at[c], v);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], add2(x[i], v[i]));
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < CH; c++) {
+                        uint64_t x[4];
+                        expand(r[c], x);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], x[i]);
                     }
@@ -418,11 +466,18 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
             }
             // the next row's loads go out before anything is stored; it is never a row that this group still has to write
             if (m + RPB < r1) fetch(m + RPB);
-            if (prm.H) {
+            auto store_row = [&](T *row) {
+                if (prm.ragged) {
 #pragma unroll
-                for (int c = 0; c < CH; c++)
-                    if (valid && col[c] < C) store_chunk(static_cast<T *>(prm.H) + m * prm.ldh, col[c], C, h[c]);
-            }
+                    for (int c = 0; c < CH; c++)
+                        if (valid && col[c] < C) store_chunk(row, col[c], C, h[c]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < CH; c++)
+                        if (valid && col[c] < C) store_whole(row + col[c], h[c]);
+                }
+            };
+            if (prm.H) store_row(static_cast<T *>(prm.H) + m * prm.ldh);
             if (CODES || prm.O) {
                 if (prm.ragged) {
 #pragma unroll
@@ -437,42 +492,65 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
                         if (k < C) make_pre(prm, vec, sample, k);
                     }
                 }
+                const float *va = vec + prm.sm_at[kA], *vb = vec + prm.sm_at[kB];
+                const int with = prm.has >> kA & 3;
+                if (with == 3) {
 #pragma unroll
-                for (int c = 0; c < CH; c++) {
-                    if (!valid || col[c] >= C) continue;
-                    uint64_t v[4], w[4];
-                    if ((prm.has >> kA & 3) == 3) {
-                        get8(vec + prm.sm_at[kA], prm.half, col[c], v);
-                        get8(vec + prm.sm_at[kB], prm.half, col[c], w);
+                    for (int c = 0; c < CH; c++) {
+                        uint64_t v[4], w[4];
+                        get8(va, prm.half, at[c], v);
+                        get8(vb, prm.half, at[c], w);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = fma2(h[c][i], v[i], w[i]);
-                    } else if (prm.has >> kA & 1) {
-                        get8(vec + prm.sm_at[kA], prm.half, col[c], v);
+                    }
+                } else if (with == 1) {
+#pragma unroll
+                    for (int c = 0; c < CH; c++) {
+                        uint64_t v[4];
+                        get8(va, prm.half, at[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = mul2(h[c][i], v[i]);
-                    } else if (prm.has >> kB & 1) {
-                        get8(vec + prm.sm_at[kB], prm.half, col[c], v);
+                    }
+                } else if (with == 2) {
+#pragma unroll
+                    for (int c = 0; c < CH; c++) {
+                        uint64_t v[4];
+                        get8(vb, prm.half, at[c], v);
 #pragma unroll
                         for (int i = 0; i < 4; i++) h[c][i] = add2(h[c][i], v[i]);
                     }
-                    if (!CODES) {
-                        store_chunk(static_cast<T *>(prm.O) + m * prm.ldo, col[c], C, h[c]);
+                }
+                if (!CODES) {
+                    store_row(static_cast<T *>(prm.O) + m * prm.ldo);
+                } else {
+                    uint8_t *rp = prm.c_pos + m * prm.ldc, *rn = DUAL ? prm.c_neg + m * prm.ldc : nullptr;
+                    auto fast = [&](int c) {
+                        const int p = int(seg[c] & 0x7FFFFFFFu);
+                        const SegConst cp = sm_pos[p], cn = DUAL ? sm_neg[p] : cp;
+                        float a[4], b[4];
+                        unpack2(h[c][0], a[0], a[1]), unpack2(h[c][1], a[2], a[3]);
+                        unpack2(h[c][2], b[0], b[1]), unpack2(h[c][3], b[2], b[3]);
+                        uint32_t wp[2], wn[2];
+                        quant4<CODE, MODE>(a, cp, cn, float(prm.hi), 0, wp[0], wn[0]);
+                        quant4<CODE, MODE>(b, cp, cn, float(prm.hi), 0, wp[1], wn[1]);
+                        if (valid && col[c] < C) {
+                            *reinterpret_cast<uint2 *>(rp + col[c]) = make_uint2(wp[0], wp[1]);
+                            if (DUAL) *reinterpret_cast<uint2 *>(rn + col[c]) = make_uint2(wn[0], wn[1]);
+                        }
+                    };
+                    if (all_fast) {
+#pragma unroll
+                        for (int c = 0; c < CH; c++) fast(c);
                     } else {
-                        uint8_t *dp = prm.c_pos + m * prm.ldc + col[c], *dn = DUAL ? prm.c_neg + m * prm.ldc + col[c] : nullptr;
-                        if (seg[c] >> 31) {
-                            Eight e;
-                            singles(h[c], e.v);
-                            codes_tail<CODE, MODE>(prm, col[c], e, dp, dn);
-                        } else {
-                            const SegConst cp = sm_pos[seg[c]], cn = DUAL ? sm_neg[seg[c]] : cp;
-                            float a[4], b[4];
-                            unpack2(h[c][0], a[0], a[1]), unpack2(h[c][1], a[2], a[3]);
-                            unpack2(h[c][2], b[0], b[1]), unpack2(h[c][3], b[2], b[3]);
-                            uint32_t wp[2], wn[2];
-                            quant4<CODE, MODE>(a, cp, cn, float(prm.hi), 0, wp[0], wn[0]);
-                            quant4<CODE, MODE>(b, cp, cn, float(prm.hi), 0, wp[1], wn[1]);
-                            *reinterpret_cast<uint2 *>(dp) = make_uint2(wp[0], wp[1]);
-                            if (DUAL) *reinterpret_cast<uint2 *>(dn) = make_uint2(wn[0], wn[1]);
+#pragma unroll
+                        for (int c = 0; c < CH; c++) {
+                            if (!(seg[c] >> 31)) {
+                                fast(c);
+                            } else if (valid && col[c] < C) {
+                                Eight e;
+                                singles(h[c], e.v);
+                                codes_tail<CODE, MODE>(prm, col[c], e, rp + col[c], DUAL ? rn + col[c] : nullptr);
+                            }
                         }
                     }
                 }
@@ -494,7 +572,8 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
     int dev = -1, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return SQ_ERR_CUDA;
-    const int pitch = (p.C + 7) / 8 * 8;                 // floats of a vector in shared memory
+    const int pitch = (p.C + 7) / 8 * 8 + 8;             // floats of a vector in shared memory
+    p.pitch = pitch;
     int vectors = 0;
     p.half = pitch / 2;
     for (int i = 0; i < 4; i++)
