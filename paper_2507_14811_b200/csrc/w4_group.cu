@@ -481,12 +481,6 @@ __device__ __forceinline__ uint32_t shared_u32(uint32_t at)
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
     return v;
 }
-__device__ __forceinline__ uint32_t shared_u16(uint32_t at)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
-    return v;
-}
 __device__ __forceinline__ int shared_s8(uint32_t at)
 {
     int v;
@@ -581,6 +575,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
     uint32_t xb[NT];                                     // this lane's activations: column g (+ 8 per MMA), codes 8 t ..
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) xb[nt] = sm0 + prm.x_off + min(g + 8 * nt, prm.cols - 1) * 64 + t * 16;
+    const uint32_t s_shift = prm.s_bytes == 2 && g % 2 == 0 ? 16 : 0, s_mask = prm.s_bytes == 2 ? 0xFFFF0000u : 0xFFFFFFFFu;
     const uint32_t x_pair = prm.cols * 64;               // 64 codes of all columns
     const uint32_t s_step = prm.unit_groups == GB ? 16 * prm.s_bytes : 0, z_step = prm.unit_groups == GB ? 16 : 0;
 
@@ -778,7 +773,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             issue(slot == 0 ? prm.stages - 1 : slot - 1);   // the stage that was used up last
             const uint32_t st = ring + slot * prm.stage_bytes, x_unit = uint32_t(u) * 4 * x_pair;
             const uint32_t f_at = sm0 + prm.f_off + (u * prm.cols8 + 2 * t) * 4, xs_at = sm0 + prm.xs_off + (u * GB * prm.cols8 + 2 * t) * 4;
-            const uint32_t s_at = st + kUnitBytes + g * prm.s_bytes, z_at = st + prm.z_off + g;
+            const uint32_t s_at = st + kUnitBytes + (g * prm.s_bytes & ~3), z_at = st + prm.z_off + g;
             int sum[NT][4];
             float part[NT][4];
             // what the sums of block b start from
@@ -795,12 +790,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             };
             // and what becomes of them
             auto finish = [&](int b) {
-                float s0, s1;
-                if (prm.s_bytes == 4) {
-                    s0 = __uint_as_float(shared_u32(s_at + b * s_step)), s1 = __uint_as_float(shared_u32(s_at + b * s_step + 32));
-                } else {
-                    s0 = __uint_as_float(shared_u16(s_at + b * s_step) << 16), s1 = __uint_as_float(shared_u16(s_at + b * s_step + 16) << 16);
-                }
+                // an fp32 scale, or one half of the word that a bf16 one lies in; without a branch, which would keep the blocks apart
+                const float s0 = __uint_as_float(shared_u32(s_at + b * s_step) << s_shift & s_mask);
+                const float s1 = __uint_as_float(shared_u32(s_at + b * s_step + 8 * prm.s_bytes) << s_shift & s_mask);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
 #pragma unroll
