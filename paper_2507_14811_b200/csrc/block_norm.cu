@@ -562,7 +562,8 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
 }
 
 // One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1280 bf16 (1024 fp32) channels
-// where there are at least five per SM, two and four up to 4096, then a block per row; fewer rows get a block each.  Rows of up to 128
+// where there are at least five per SM, two, four and eight up to 8192, then a block per row; fewer rows get a block each.  (2048 x 5120:
+// 35 us with a block per row, 20.5 with two rows a block, which share their vectors.)  Rows of up to 128
 // channels take 8 or 16 lanes (32768 x 64: 14.1 -> 5.5 us).  Samples of fewer than 16 rows: every row makes its vectors (16384 x 640, a vector
 // per row: 93.7 us with a block per row, 51.4 with a warp).  (8858 x 1536 bf16 to codes: one warp with six chunks a lane, held to 128 registers, 28.1 us; two with three
 // 23.1 us.  32768 x 1280: one warp with five chunks 55.8 us, two with three, of which one sixth is idle, 63.2 us.)
@@ -633,6 +634,8 @@ sq_status run_shape(BlockNormParams p, cudaStream_t st)
         if (chunks <= 192) SQ_SHARED(3, 2, 4, HALF ? 3 : 2, 32);
         if (chunks <= 256) SQ_SHARED(4, 2, 4, 2, 32);
         if (chunks <= 512) SQ_SHARED(4, 4, 2, 2, 32);
+        if (chunks <= 768) SQ_SHARED(3, 8, 2, 1, 32);
+        if (chunks <= 1024) SQ_SHARED(4, 8, 2, 1, 32);
     }
     if (p.M >= int64_t(sms) * 2) {
         if (chunks <= 128) SQ_ROW(1, 4, 6);

@@ -175,6 +175,11 @@ CASES = [
     (1184, 3080, 1184, BF, BF, "rms", "rms", ("post_w", "w"), True, True, False),
     (1184, 1500, 592, BF, BF, "layer", "layer", ALL, True, True, False),
     (1250, 6000, 1250, BF, BF, "rms", "rms", ("post_w", "w"), True, True, False),
+    (760, 8001, 100, BF, F32, "layer", "layer", ALL, True, True, True),
+    (801, 5000, 401, F32, F32, "none", "layer", ("gate", "scale", "shift"), True, True, False),
+    (750, 5000, 2, BF, BF, "rms", "layer", ALL, True, True, False),
+    (400, 6000, 200, BF, BF, "none", "layer", ("gate", "scale", "shift"), True, True, False),
+    (300, 12000, 300, F32, BF, "rms", "layer", ALL, True, True, False),
 ]
 
 
