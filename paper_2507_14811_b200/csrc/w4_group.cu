@@ -661,7 +661,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                         copy16(dst + (i & 1 ? d1 : d0) + (i >> 1) * 1024, in ? p + i * row4 : prm.W4, in ? bytes : 0);
                     }
                     if (s_lane) {
-                        const int rest = (prm.N - n0 - s_n) * prm.s_bytes;
+                        const int rest = min(prm.N - n0 - s_n, 16) * prm.s_bytes;
                         const bool in = g0 + s_group < prm.groups && rest > 0;
                         copy16(dst + kUnitBytes + lane * 16, in ? s_src + g0 * prm.lds : prm.s, in ? min(16, rest) : 0);
                     }

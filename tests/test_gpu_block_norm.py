@@ -301,6 +301,18 @@ def test_broadcast_vectors():
         assert torch.equal(H, outs[0][0]) and torch.equal(O, outs[0][1])
 
 
+def test_a_copy_of_the_stream():
+    """H given without Y: the residual stream is stored there as it is, with and without an output."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    for M, C in ((5, 301), (1300, 301)):
+        R = rows(g, M, C, BF)
+        H = torch.zeros((M, 304), dtype=BF, device=DEV)[:, :C]
+        got, O = B.segquant_block_norm(R, H=H)
+        assert got is H and torch.equal(H, R) and torch.equal(O, B.segquant_block_norm(R)[1])
+        H.zero_()
+        assert B.segquant_block_norm(R, H=H, store_out=False)[1] is None and torch.equal(H, R)
+
+
 def test_offsets_beyond_32_bits():
     M, C = 140000, 16384                                     # 4.6 GB of bf16
     R = torch.zeros((M, C), dtype=BF, device=DEV)
