@@ -514,6 +514,10 @@ __device__ __forceinline__ float largest(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
     return d;
 }
+__device__ __forceinline__ float largest8(const float (&x)[8])
+{
+    return largest(largest(largest(x[0], x[1]), largest(x[2], x[3])), largest(largest(x[4], x[5]), largest(x[6], x[7])));
+}
 __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -712,10 +716,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) unpack2(silu2(x[j], x[j + 1]), x[j], x[j + 1]);
                 } else if (prm.act == SQ_ACT_GELU) {
+                    const float in = largest8(x);
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) unpack2(gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                    if (!(in < __uint_as_float(0x7F800000u))) x[0] = in;                // (it makes 0 of a NaN and of -infinity)
                 }
-                float top = largest(largest(largest(x[0], x[1]), largest(x[2], x[3])), largest(largest(x[4], x[5]), largest(x[6], x[7])));
+                float top = largest8(x);
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                 const bool finite = top < __uint_as_float(0x7F800000u);
