@@ -314,8 +314,9 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     longer one) are exact, the rest is fp32 in an order that depends on the sizes and the device alone; one
  *     rounding to y_dtype.  A row with an infinity or a NaN in X has NaN for outputs, whatever act makes of it.  X [M,K] dev (dtype dt, ldx
  *     elements), bias dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements
- *     only; Y must not overlap X, bias or Wq4.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072, M <= 65535,
+ *     only; Y must not overlap X, bias, Wq4, s_w or z_w.  Codes of any 4 bits, zero-points in [-8, 7].  K <= 131072, M <= 65535,
  *     meant for M of at most about 32 (the weights are read once per pass of up to 10 rows).  No workspace.
+ *   The quantizer's outputs must not overlap W or one another, the dequantizer's W not Wq4, s_w or z_w (SQ_ERR_UNSUPPORTED).
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
  *     N <= 4194240 for segquant_dequantize_w4_group. */
 sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int64_t K, int64_t ld, int64_t group, void *Wq4,
@@ -341,7 +342,7 @@ sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, i
  *     without its output in device memory.  The quotient o / s carries the fp32 error of o, so a code may be the neighbouring one
  *     where the exact quotient lies that close to a rounding boundary.
  *   Y, R, H, O dev, dtype dt, pitches in elements; H and O may be Y or R themselves (same address and pitch), any other overlap
- *   of an output with an input, a vector or another output is refused with SQ_ERR_UNSUPPORTED.  Alignment: Y, R, H, O and codes 16 bytes, pitches multiples of 16 bytes; the vectors
+ *   of an output with an input, a vector, the scales or another output is refused with SQ_ERR_UNSUPPORTED.  Alignment: Y, R, H, O and codes 16 bytes, pitches multiples of 16 bytes; the vectors
  *   that of their elements.  C <= 16384.  Values beyond about 2^60 overflow the sums of squares. */
 typedef enum { SQ_NORM_NONE = 0, SQ_NORM_RMS = 1, SQ_NORM_LAYER = 2 } sq_norm;
 typedef struct {

@@ -177,6 +177,18 @@ static sq_status check_w4_group(const W4Group &w)
     return SQ_OK;
 }
 
+// Bytes from the first to the last of a weight's codes, scales and zero-points.
+static size_t codes_extent(const W4Group &w) { return size_t((w.N - 1) * w.ldw + (w.K + 1) / 2); }
+static size_t scales_extent(const W4Group &w) { return size_t(((w.K - 1) / w.group * w.lds + w.N) * int64_t(dt_size(w.s_dtype))); }
+static size_t zeros_extent(const W4Group &w) { return size_t((w.K - 1) / w.group * w.ldz + w.N); }
+
+// Whether a range shares a byte with any of them.
+static bool meets(const W4Group &w, const void *p, size_t bytes)
+{
+    return overlap(w.W4, codes_extent(w), p, bytes) || overlap(w.s, scales_extent(w), p, bytes) ||
+           (w.z && overlap(w.z, zeros_extent(w), p, bytes));
+}
+
 // ---- block norms
 constexpr int64_t kMaxNormC = 16384;      // a row is held in one thread block's registers
 
@@ -589,8 +601,11 @@ sq_status segquant_quantize_w4_group(const void *W, sq_dtype dt, int64_t N, int6
     if (!valid_dt(dt)) return SQ_ERR_UNSUPPORTED;
     sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
     if (st != SQ_OK) return st;
-    if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
-    if (overlap(W, size_t((N - 1) * ld + K) * dt_size(dt), Wq4, size_t((N - 1) * ldw + (K + 1) / 2))) return SQ_ERR_UNSUPPORTED;
+    const W4Group w{Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz};
+    if ((st = check_w4_group(w)) != SQ_OK) return st;
+    // the outputs apart from the weights and from one another
+    if (meets(w, W, size_t((N - 1) * ld + K) * dt_size(dt)) || overlap(Wq4, codes_extent(w), s_w, scales_extent(w))) return SQ_ERR_UNSUPPORTED;
+    if (z_w && (overlap(Wq4, codes_extent(w), z_w, zeros_extent(w)) || overlap(s_w, scales_extent(w), z_w, zeros_extent(w)))) return SQ_ERR_UNSUPPORTED;
     return launch_quantize_w4_group(W, dt, N, K, ld, group, Wq4, ldw, s_w, s_dtype, lds, z_w, ldz, static_cast<cudaStream_t>(stream));
 }
 
@@ -601,8 +616,9 @@ sq_status segquant_dequantize_w4_group(const void *Wq4, int64_t ldw, int64_t N, 
     if (!valid_dt(dt)) return SQ_ERR_UNSUPPORTED;
     sq_status st = check_matrix(W, N, K, ld, dt_size(dt));
     if (st != SQ_OK) return st;
-    if ((st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz})) != SQ_OK) return st;
-    if (overlap(W, size_t((N - 1) * ld + K) * dt_size(dt), Wq4, size_t((N - 1) * ldw + (K + 1) / 2))) return SQ_ERR_UNSUPPORTED;
+    const W4Group w{Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz};
+    if ((st = check_w4_group(w)) != SQ_OK) return st;
+    if (meets(w, W, size_t((N - 1) * ld + K) * dt_size(dt))) return SQ_ERR_UNSUPPORTED;
     return launch_dequantize_w4_group(Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz, W, dt, ld, static_cast<cudaStream_t>(stream));
 }
 
@@ -614,14 +630,15 @@ sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, i
     if (!valid_dt(dt) || !valid_dt(y_dtype)) return SQ_ERR_UNSUPPORTED;
     if (act != SQ_ACT_NONE && act != SQ_ACT_SILU && act != SQ_ACT_GELU) return SQ_ERR_UNSUPPORTED;
     if (M <= 0 || M > 65535 || K <= 0 || K > kMaxK || ldx < K || ldy < N) return SQ_ERR_SHAPE;
-    const sq_status st = check_w4_group({Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz});
+    const W4Group w{Wq4, ldw, N, K, group, s_w, s_dtype, lds, z_w, ldz};
+    const sq_status st = check_w4_group(w);
     if (st != SQ_OK) return st;
     const int64_t xs = int64_t(dt_size(dt)), ys = int64_t(dt_size(y_dtype));
     if (reinterpret_cast<uintptr_t>(X) % xs || reinterpret_cast<uintptr_t>(Y) % ys || (reinterpret_cast<uintptr_t>(bias) & 3u))
         return SQ_ERR_ALIGN;
     const size_t y_bytes = size_t((M - 1) * ldy + N) * ys;
     if (rows_overlap(X, ldx * xs, K * xs, Y, ldy * ys, N * ys, M) || (bias && overlap(bias, size_t(N) * 4, Y, y_bytes))) return SQ_ERR_UNSUPPORTED;
-    if (overlap(Wq4, size_t((N - 1) * ldw + (K + 1) / 2), Y, y_bytes)) return SQ_ERR_UNSUPPORTED;
+    if (meets(w, Y, y_bytes)) return SQ_ERR_UNSUPPORTED;
     return launch_w4_matvec({X, dt, M, K, ldx, act, Wq4, ldw, N, group, s_w, s_dtype, lds, z_w, ldz, bias, Y, y_dtype, ldy},
                             static_cast<cudaStream_t>(stream));
 }
@@ -655,6 +672,13 @@ sq_status segquant_block_norm_quantize(const void *Y, int64_t ldy, const void *R
     const HostSeg hs = load_segtable(seg, C, seg && seg->nb && seg->Q >= 1 ? seg->nb[seg->Q] : 0);
     if (hs.status != SQ_OK) return hs.status;
     a.sb = hs.b;
+    // nor may an output take the place of the scales
+    const size_t h_bytes = H ? (size_t(M - 1) * ldh + C) * dt_size(dt) : 0, c_bytes = size_t(M - 1) * ldc + C;
+    for (const float *v : {s_pos, s_neg}) {
+        const size_t bytes = size_t(hs.b.P) * sizeof(float);
+        if (v && (overlap(v, bytes, c_pos, c_bytes) || (s_neg && overlap(v, bytes, c_neg, c_bytes)) || (H && overlap(v, bytes, H, h_bytes))))
+            return SQ_ERR_UNSUPPORTED;
+    }
     return launch_block_norm(a, static_cast<cudaStream_t>(stream));
 }
 
