@@ -550,9 +550,10 @@ __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
 //
 // Fixed point: with 2^E <= max|x| < 2^(E+1) over the 256 inputs of a unit, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
 // 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact); the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2
-// with q = q0 + 256 q1 + 65536 q2.  A block, a group or 128 inputs of a longer one, has a sum of 16 (c - z) q_i within 2^22 for
-// zero-points in [-8, 7], so that it becomes a float by starting at the bits of 1.5 * 2^23 and subtracting that number: the start,
-// less the zero-point times the block's sum of q_i, is the MMA's addend.  One FMA in fp32 takes it with its scale to the unit's sum, and one
+// with q = q0 + 256 q1 + 65536 q2.  A block, a group or 128 inputs of a longer one, has a sum of 16 c q_i within 2^21, so that it becomes
+// a float by starting at the bits of 1.5 * 2^23, the MMA's addend, and subtracting that number.  One FMA takes off the zero-point times the
+// block's sum of 16 q_i (both are whole numbers of fp32; their product and the difference are, too, for zero-points in [-8, 7], and are rounded
+// once beyond; as the MMA's addend they would leave the range of the start for those).  One FMA takes it with its scale to the unit's sum, and one
 // the unit's sum with 2^(E - 25) 256^i to the tile's.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
 // instead of one per unit: 26.3 us against 25.8 for 1 x 8192 -> 28672, 9.7 against 8.8 for 8 x 1536 -> 9216 with SiLU.)
 // GB: blocks of a unit (2, 4, 8).
@@ -748,9 +749,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                         for (int p = 0; p < 3; p++) sum[p] += __shfl_xor_sync(0xFFFFFFFFu, sum[p], d);
                     }
                     if (lane % kBlockLanes == 0) {
-                        int *xs = reinterpret_cast<int *>(smem + prm.xs_off) + e / kBlockLanes * prm.cols8 + m;
+                        float *xs = reinterpret_cast<float *>(smem + prm.xs_off) + e / kBlockLanes * prm.cols8 + m;
 #pragma unroll
-                        for (int p = 0; p < 3; p++) xs[p * prm.rows] = 16 * sum[p];
+                        for (int p = 0; p < 3; p++) xs[p * prm.rows] = float(16 * sum[p]);
                     }
                 }
                 if (lane < 3) {
@@ -766,11 +767,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
         int slot = 0, tile = 0, u = 0;
         if (end > begin) tile = begin / U, u = begin - tile * U;
         float *to = u == 0 ? red + tile * (prm.cols * kRedPitch) : head + warp * (prm.cols * kRedPitch);
-        float acc[NT][4];
+        uint64_t acc[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) acc[nt][i] = 0.0f;
+        for (int nt = 0; nt < NT; nt++) acc[nt][0] = acc[nt][1] = 0;
         for (int i = begin; i < end; i++) {
             if (prm.stages == 4) copies_wait<2>();
             else if (prm.stages == 3) copies_wait<1>();
@@ -781,30 +780,34 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             const uint32_t f_at = sm0 + prm.f_off + (u * prm.cols8 + 2 * t) * 4, xs_at = sm0 + prm.xs_off + (u * GB * prm.cols8 + 2 * t) * 4;
             const uint32_t s_at = st + kUnitBytes + (g * prm.s_bytes & ~3), z_at = st + prm.z_off + g;
             int sum[NT][4];
-            float part[NT][4];
-            // what the sums of block b start from
-            auto start = [&](int b) {
-                int z0 = 0, z1 = 0;
-                if (ZP) z0 = shared_s8(z_at + b * z_step), z1 = shared_s8(z_at + b * z_step + 8);
+            uint64_t part[NT][2];                        // two columns at a time
+            // what the sums of a block start from
+            auto start = [&]() {
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    uint2 xs = make_uint2(0u, 0u);
-                    if (ZP) xs = shared_v2(xs_at + (b * prm.cols8 + nt * 8) * 4);
-                    sum[nt][0] = kMagicBits - z0 * int(xs.x), sum[nt][1] = kMagicBits - z0 * int(xs.y);
-                    sum[nt][2] = kMagicBits - z1 * int(xs.x), sum[nt][3] = kMagicBits - z1 * int(xs.y);
-                }
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) sum[nt][j] = kMagicBits;
             };
-            // and what becomes of them
+            // and what becomes of those of block b
             auto finish = [&](int b) {
                 // an fp32 scale, or one half of the word that a bf16 one lies in; without a branch, which would keep the blocks apart
                 const float s0 = __uint_as_float(shared_u32(s_at + b * s_step) << s_shift & s_mask);
                 const float s1 = __uint_as_float(shared_u32(s_at + b * s_step + 8 * prm.s_bytes) << s_shift & s_mask);
+                float z0 = 0.0f, z1 = 0.0f;              // -z
+                if (ZP) {
+                    z0 = kRoundMagic - __int_as_float(kMagicBits + shared_s8(z_at + b * z_step));
+                    z1 = kRoundMagic - __int_as_float(kMagicBits + shared_s8(z_at + b * z_step + 8));
+                }
+                const uint64_t sc[2] = {pack2(s0, s0), pack2(s1, s1)}, z[2] = {pack2(z0, z0), pack2(z1, z1)};
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
+                    uint2 xs = make_uint2(0u, 0u);
+                    if (ZP) xs = shared_v2(xs_at + (b * prm.cols8 + nt * 8) * 4);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const float v = __int_as_float(sum[nt][j]) - kRoundMagic, sc = j < 2 ? s0 : s1;
-                        part[nt][j] = b == 0 ? sc * v : fmaf(sc, v, part[nt][j]);
+                    for (int j = 0; j < 2; j++) {
+                        uint64_t v = add2(pack2(__int_as_float(sum[nt][2 * j]), __int_as_float(sum[nt][2 * j + 1])), pack2(-kRoundMagic, -kRoundMagic));
+                        if (ZP) v = fma2(z[j], pack2(__uint_as_float(xs.x), __uint_as_float(xs.y)), v);
+                        part[nt][j] = b == 0 ? mul2(sc[j], v) : fma2(sc[j], v, part[nt][j]);
                     }
                 }
             };
@@ -816,10 +819,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 uint4 x[NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) x[nt] = shared_v4(xb[nt] + x_unit + pr * x_pair);
-                if (GB == 8 || GB == 4 || pr % 2 == 0) start(GB == 2 ? pr / 2 : GB == 4 ? pr : 2 * pr);
+                if (GB == 8 || GB == 4 || pr % 2 == 0) start();
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) mma(sum[nt], w[0] << 4 & high, w[1] << 4 & high, w[0] & high, w[1] & high, x[nt].x, x[nt].y, sum[nt]);
-                if (GB == 8) finish(2 * pr), start(2 * pr + 1);
+                if (GB == 8) finish(2 * pr), start();
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) mma(sum[nt], w[2] << 4 & high, w[3] << 4 & high, w[2] & high, w[3] & high, x[nt].z, x[nt].w, sum[nt]);
                 if (GB == 8) finish(2 * pr + 1);
@@ -830,17 +833,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
             for (int nt = 0; nt < NT; nt++) {
                 const uint2 f = shared_v2(f_at + nt * 32);
 #pragma unroll
-                for (int j = 0; j < 4; j++) acc[nt][j] = fmaf(__uint_as_float(j % 2 ? f.y : f.x), part[nt][j], acc[nt][j]);
+                for (int j = 0; j < 2; j++) acc[nt][j] = fma2(pack2(__uint_as_float(f.x), __uint_as_float(f.y)), part[nt][j], acc[nt][j]);
             }
             slot = slot + 1 == prm.stages ? 0 : slot + 1;
             if (++u == U || i + 1 == end) {              // what this run has of the tile: [column][16 channels]
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const int col = nt * 8 + 2 * t + (j & 1);
-                        if (col < prm.cols) to[col * kRedPitch + g + (j >> 1) * 8] = acc[nt][j];
-                        acc[nt][j] = 0.0f;
+                    for (int j = 0; j < 2; j++) {
+                        const int col = nt * 8 + 2 * t;
+                        float a, b;
+                        unpack2(acc[nt][j], a, b);
+                        if (col < prm.cols) to[col * kRedPitch + g + j * 8] = a;
+                        if (col + 1 < prm.cols) to[(col + 1) * kRedPitch + g + j * 8] = b;
+                        acc[nt][j] = 0;
                     }
                 }
                 u = 0, tile++;

@@ -1,13 +1,39 @@
-"""The matrix-vector product with 4-bit weights at the ends of its ranges: activations that are no numbers behind an activation function."""
+"""The matrix-vector product with 4-bit weights at the ends of its ranges: activations that are no numbers behind an activation function,
+zero-points anywhere in int8.
+
+Tolerances.  u = 2^-24 is a rounding's share.  A term of a sum is on its way through at most 50 + ceil(K / 256) roundings: the zero-point's and the
+scale's multiply-add, up to eight blocks of a unit, the units, then sixteen runs, the bytes, lanes, eight CTAs and the bias.  The bytes that an
+activation is split into are at most 3.03 times as large together as the activation: those below the leading one, 256^p of which the
+activation has at least half of, add up to at most 0.502 of 256^p, and the leading one is off the activation by that much again.
+An activation is off by at most 2^-22 of the largest magnitude of its row in its 256 inputs, or 2^-123.  bf16 outputs are rounded once more, by at
+most half a step."""
 import pytest
 import torch
 
 from paper_2507_14811_b200 import binding as B
-from test_gpu_w4_group import random_codes
+from test_gpu_w4_group import act64, act_error, random_codes, weights64
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 BF, F32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24
+
+
+def check(Y, X, W, K, act=None, fixed=2.0 ** -22, error=act_error):
+    """fixed: an activation's error relative to the largest; error(x, act): the activation function's."""
+    x = X.double()
+    a = act64(x, act)
+    of_act = a.abs() * error(x, act)
+    pad = torch.zeros((a.shape[0], -(-K // 256) * 256), dtype=torch.float64, device=DEV)
+    pad[:, :K] = a.abs() + of_act
+    largest = pad.view(a.shape[0], -1, 256).amax(2).repeat_interleave(256, 1)[:, :K]
+    off = (of_act + fixed * largest + 2.0 ** -123) * (a != 0)
+    want = a @ W.t()
+    tol = off @ W.abs().t() + (50 + -(-K // 256)) * U * 3.03 * ((a.abs() + off) @ W.abs().t()) + 2.0 ** -140
+    if Y.dtype == BF:
+        tol = tol + 2.0 ** -8 * (want.abs() + tol)
+    err = (Y.double() - want).abs()
+    assert bool(torch.all(err <= tol)), f"worst {float((err / tol).max()):.3g} of the tolerance"
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -26,3 +52,26 @@ def test_what_is_no_number_stays_none_behind_an_activation(x, y, act):
         assert torch.equal(got[m], clean[m])
     for m in (1, 4, 5, 7):
         assert bool(torch.isnan(got[m]).all()), m
+
+
+@pytest.mark.parametrize("M,K,N,G,x,y", [
+    (1, 1111, 77, 32, BF, F32), (3, 1000, 130, 64, F32, F32), (8, 2048, 300, 128, BF, BF), (9, 900, 64, 256, BF, F32), (6, 700, 48, 512, F32, F32)])
+def test_any_zero_point(M, K, N, G, x, y):
+    """Matrices packed elsewhere may have zero-points anywhere in int8."""
+    W4, s_w, _ = random_codes(N, K, G, False, F32, 11)
+    z_w = torch.randint(-128, 128, (s_w.shape[0], -(-N // 16) * 16), device=DEV, dtype=torch.int8)[:, :N]
+    z_w[0, 0], z_w[0, 1] = -128, 127
+    g = torch.Generator(device=DEV).manual_seed(12)
+    X = (torch.rand((M, K), generator=g, device=DEV) + 0.5).to(x)            # (one sign: large sums)
+    Y = B.segquant_w4_matvec(X, W4, s_w, G, z_w, y_dtype=y)
+    check(Y, X, weights64(W4, s_w, z_w, G, K), K)
+
+
+def test_zero_points_of_weights_next_to_nothing():
+    """Ranges of a few subnormal steps: the quantizer's own zero-points go beyond [-8, 7] there, because its scale is a whole number of steps."""
+    W = torch.full((16, 128), -22 * 2.0 ** -149)
+    W4, s_w, z_w = B.segquant_quantize_w4_group(W.to(DEV), 128, F32, True)
+    assert int(z_w.max()) > 7
+    X = torch.full((2, 128), float(0x3F7F7F) * 2.0 ** 78, device=DEV)          # (bytes as large as they get)
+    for y in (BF, F32):
+        check(B.segquant_w4_matvec(X, W4, s_w, 128, z_w, y_dtype=y), X, weights64(W4, s_w, z_w, 128, 128), 128)
