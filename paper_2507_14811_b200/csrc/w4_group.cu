@@ -7,7 +7,7 @@
 // instructions per code, and half of that on either arithmetic pipe, so codes are not turned into real numbers one by one.  A byte of
 // two codes is two signed bytes 16 c after one mask each (0.4 instructions per code), which integer matrix instructions take as they are:
 // mma.m16n8k32, 16 channels on its rows.  The activations become 23-bit fixed-point numbers, as three signed bytes in three of
-// its 8 columns; products and a group's sums are exact integers, and scales and zero-points come in behind a group.
+// its 8 columns (38 bits in five, where fp32 activations make fp32 outputs); products and a group's sums are exact integers, and scales and zero-points come in behind a group.
 // (Expanded to bf16 instead, 1.4 instructions per code, the same design took 38.3 us for 1 x 8192 -> 28672 with zero-points.)  tcgen05
 // would want the expanded codes in shared memory, twice the bytes that came in, and has nothing to offer: the tensor pipe is no bound here.
 #include <cuda_bf16.h>
@@ -420,7 +420,7 @@ constexpr int kUnitK = 256;          // codes per channel and ring stage: 128 by
 constexpr int kUnitBytes = kTileN * kUnitK / 2;
 constexpr int kMaxStages = 4;        // of a warp's ring; 2 or 3 where the activations leave no room for more
 constexpr int kRedPitch = 20;        // floats per column of a tile's sums (16 used; 20 keeps the stores off one bank)
-constexpr int kMaxCols = 32;         // columns of a pass: 10 rows of three bytes each
+constexpr int kMaxCols = 32;         // columns of a pass: 10 rows of three bytes each, 6 of five
 constexpr int kAhead = 3;            // loads of eight activations that a thread has in flight
 constexpr int kMaxBlock = 128;       // inputs of an exact sum: a group, or this many of a longer one
 
@@ -449,7 +449,8 @@ struct MatvecParams {
     int units, units_cta;            // of K, of a CTA
     int tiles, clusters;
     int tiles_round;                 // tiles whose sums fit in shared memory
-    int cols, cols8;                 // columns in use, 3 * rows; rounded up to whole MMAs
+    int parts;                       // bytes of an activation, 3 or 5
+    int cols, cols8;                 // columns in use, parts * rows; rounded up to whole MMAs
     int stages;
     uint32_t stage_bytes, z_off, x_off, f_off, xs_off, red_off, head_off, out_off;
 };
@@ -549,15 +550,18 @@ __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
 // of K will do as long as both operands have it.
 //
 // Fixed point: with 2^E <= max|x| < 2^(E+1) over the 256 inputs of a unit, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
-// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact); the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2
-// with q = q0 + 256 q1 + 65536 q2.  A block, a group or 128 inputs of a longer one, has a sum of 16 c q_i within 2^21, so that it becomes
+// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact, and behind a bf16 rounding of the outputs the others are good enough); the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2
+// with q = q0 + 256 q1 + 65536 q2.  fp32 outputs of fp32 activations, or of an activation function's values, are to have the digits of fp32
+// products: round(2^15 (x 2^(21 - E) - q)) follows in two more bytes, off by at most 2^-37 of the maximum (an fp32 x down to 2^-13 of it
+// is exact).  The rule looks at types alone.  (Three bytes there: an input in 256 a thousand times the others, weights of theirs
+// a thousand times its own: 4.9e-5 of the output instead of 2e-7.)  A block, a group or 128 inputs of a longer one, has a sum of 16 c q_i within 2^21, so that it becomes
 // a float by starting at the bits of 1.5 * 2^23, the MMA's addend, and subtracting that number.  One FMA takes off the zero-point times the
 // block's sum of 16 q_i (both are whole numbers of fp32; their product and the difference are, too, for zero-points in [-8, 7], and are rounded
 // once beyond; as the MMA's addend they would leave the range of the start for those).  One FMA takes it with its scale to the unit's sum, and one
 // the unit's sum with 2^(E - 25) 256^i to the tile's.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
 // instead of one per unit: 26.3 us against 25.8 for 1 x 8192 -> 28672, 9.7 against 8.8 for 8 x 1536 -> 9216 with SiLU.)
-// GB: blocks of a unit (2, 4, 8).
-template <int NT, int GB, bool ZP>
+// GB: blocks of a unit (2, 4, 8).  PARTS: bytes of an activation (3, 5).
+template <int NT, int GB, bool ZP, int PARTS>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_constant__ MatvecParams prm)
 {
     extern __shared__ __align__(128) uint8_t smem[];
@@ -726,37 +730,52 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                 const bool finite = top < __uint_as_float(0x7F800000u);
-                const uint32_t be = max(__float_as_uint(top) >> 23, 27u);               // biased E; smaller ranges count as 2^-100
+                const uint32_t be = max(__float_as_uint(top) >> 23, PARTS == 5 ? 41u : 26u);     // biased E; smaller ranges count as 2^-86, 2^-101
                 const float up = finite ? __uint_as_float((275u - be) << 23) : 0.0f;    // 2^(21 - E); (other blocks: any bytes)
-                uint32_t v[8];
-#pragma unroll
-                for (int j = 0; j < 8; j++) v[j] = __float_as_uint(fmaf(x[j], up, kRoundMagic)) - (0x4B400000u - 0x8080u);
                 uint8_t *dst = smem + prm.x_off + size_t(e >> 3) * x_pair + (e & 3) * 16 + (e >> 2 & 1) * 8;
-                uint32_t even[3], odd[3];
-                bytes_of(v[0], v[2], v[4], v[6], even);
-                bytes_of(v[1], v[3], v[5], v[7], odd);
-                int sum[3] = {0, 0, 0};
+                // the lower COUNT bytes of v, the uppermost as it is if it is the number's own, to columns p, p + 1, ..
+                auto put = [&](const uint32_t (&v)[8], int p0, auto count) {
+                    constexpr int COUNT = decltype(count)::value;
+                    uint32_t even[3], odd[3];
+                    bytes_of(v[0], v[2], v[4], v[6], even);
+                    bytes_of(v[1], v[3], v[5], v[7], odd);
+                    int sum[COUNT];
 #pragma unroll
-                for (int p = 0; p < 3; p++) {
-                    const uint2 b2 = p < 2 ? make_uint2(even[p] ^ 0x80808080u, odd[p] ^ 0x80808080u) : make_uint2(even[p], odd[p]);
-                    *reinterpret_cast<uint2 *>(dst + (p * prm.rows + m) * 64) = b2;
-                    if (ZP) sum[p] = __dp4a(int(b2.x), 0x01010101, __dp4a(int(b2.y), 0x01010101, 0));
-                }
-                if (ZP) {
-#pragma unroll
-                    for (int d = 1; d < kBlockLanes; d <<= 1) {
-#pragma unroll
-                        for (int p = 0; p < 3; p++) sum[p] += __shfl_xor_sync(0xFFFFFFFFu, sum[p], d);
+                    for (int p = 0; p < COUNT; p++) {
+                        const uint2 b2 = p < 2 ? make_uint2(even[p] ^ 0x80808080u, odd[p] ^ 0x80808080u) : make_uint2(even[p], odd[p]);
+                        *reinterpret_cast<uint2 *>(dst + ((p0 + p) * prm.rows + m) * 64) = b2;
+                        if (ZP) sum[p] = __dp4a(int(b2.x), 0x01010101, __dp4a(int(b2.y), 0x01010101, 0));
                     }
-                    if (lane % kBlockLanes == 0) {
-                        float *xs = reinterpret_cast<float *>(smem + prm.xs_off) + e / kBlockLanes * prm.cols8 + m;
+                    if (ZP) {
 #pragma unroll
-                        for (int p = 0; p < 3; p++) xs[p * prm.rows] = float(16 * sum[p]);
+                        for (int d = 1; d < kBlockLanes; d <<= 1) {
+#pragma unroll
+                            for (int p = 0; p < COUNT; p++) sum[p] += __shfl_xor_sync(0xFFFFFFFFu, sum[p], d);
+                        }
+                        if (lane % kBlockLanes == 0) {
+                            float *xs = reinterpret_cast<float *>(smem + prm.xs_off) + e / kBlockLanes * prm.cols8 + m;
+#pragma unroll
+                            for (int p = 0; p < COUNT; p++) xs[(p0 + p) * prm.rows] = float(16 * sum[p]);
+                        }
                     }
+                };
+                constexpr uint32_t offset = 0x4B400000u - 0x8080u;
+                uint32_t v[8];
+                if constexpr (PARTS == 5) {
+#pragma unroll
+                    for (int j = 0; j < 8; j++) {
+                        const float q = fmaf(x[j], up, kRoundMagic) - kRoundMagic, rest = fmaf(x[j], up, -q);      // (both exact)
+                        v[j] = __float_as_uint(fmaf(rest, 32768.0f, kRoundMagic)) - offset;
+                    }
+                    put(v, 0, std::integral_constant<int, 2>());
                 }
-                if (lane < 3) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = __float_as_uint(fmaf(x[j], up, kRoundMagic)) - offset;
+                put(v, PARTS - 3, std::integral_constant<int, 3>());
+                if (lane < PARTS) {
                     float *f = reinterpret_cast<float *>(smem + prm.f_off) + (e >> 5) * prm.cols8 + m;
-                    f[lane * prm.rows] = finite ? __uint_as_float((be - 25u + 8u * lane) << 23) : __uint_as_float(0x7FC00000u);
+                    const int exponent = int(be) - 25 + (lane < PARTS - 3 ? 8 * lane - 15 : 8 * (lane - (PARTS - 3)));
+                    f[lane * prm.rows] = finite ? __uint_as_float(uint32_t(exponent) << 23) : __uint_as_float(0x7FC00000u);
                 }
             }
             __syncthreads();
@@ -879,7 +898,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 for (int w = w_first + j; w <= w_last; w += 1 << share) {
                     if (w * total / kWarps == (w + 1) * total / kWarps) continue;     // a run of nothing (fewer units than warps)
                     const float *from = (w == w_first ? red + tl * (prm.cols * kRedPitch) : head + w * (prm.cols * kRedPitch)) + m * kRedPitch + c;
-                    v += from[0] + from[prm.rows * kRedPitch] + from[2 * prm.rows * kRedPitch];
+                    float bytes = from[0];
+                    for (int p = 1; p < PARTS; p++) bytes += from[p * prm.rows * kRedPitch];
+                    v += bytes;
                 }
             }
             for (int d = 1; d < 1 << share; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
@@ -910,24 +931,29 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 
 // ---------------------------------------------------------------------------------------------- host side
 
-template <int NT, bool ZP>
+template <int NT, bool ZP, int PARTS>
 const void *matvec_kernel(int gb)
 {
     switch (gb) {
-        case 2: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 2, ZP>);
-        case 4: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 4, ZP>);
-        default: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 8, ZP>);
+        case 2: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 2, ZP, PARTS>);
+        case 4: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 4, ZP, PARTS>);
+        default: return reinterpret_cast<const void *>(w4_matvec_kernel<NT, 8, ZP, PARTS>);
     }
 }
 constexpr int kMaxNt = kMaxCols / 8;
+template <int PARTS>
 const void *matvec_kernel(int nt, int gb, bool zp)
 {
     switch (nt) {
-        case 1: return zp ? matvec_kernel<1, true>(gb) : matvec_kernel<1, false>(gb);
-        case 2: return zp ? matvec_kernel<2, true>(gb) : matvec_kernel<2, false>(gb);
-        case 3: return zp ? matvec_kernel<3, true>(gb) : matvec_kernel<3, false>(gb);
-        default: return zp ? matvec_kernel<4, true>(gb) : matvec_kernel<4, false>(gb);
+        case 1: return zp ? matvec_kernel<1, true, PARTS>(gb) : matvec_kernel<1, false, PARTS>(gb);
+        case 2: return zp ? matvec_kernel<2, true, PARTS>(gb) : matvec_kernel<2, false, PARTS>(gb);
+        case 3: return zp ? matvec_kernel<3, true, PARTS>(gb) : matvec_kernel<3, false, PARTS>(gb);
+        default: return zp ? matvec_kernel<4, true, PARTS>(gb) : matvec_kernel<4, false, PARTS>(gb);
     }
+}
+const void *matvec_kernel(int nt, int gb, bool zp, int parts)
+{
+    return parts == 5 ? matvec_kernel<5>(nt, gb, zp) : matvec_kernel<3>(nt, gb, zp);
 }
 
 // Per device: SM count, and the clusters of 2, 4 and 8 CTAs that are resident at once (GPCs have different numbers of SMs).
@@ -950,7 +976,8 @@ sq_status matvec_device(MatvecDevice *out)
     for (int nt = 1; nt <= kMaxNt && e == cudaSuccess; nt++)
         for (int gb = 2; gb <= 8 && e == cudaSuccess; gb *= 2)
             for (int zp = 0; zp < 2 && e == cudaSuccess; zp++)
-                e = cudaFuncSetAttribute(matvec_kernel(nt, gb, zp), cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem));
+                for (int parts = 3; parts <= 5 && e == cudaSuccess; parts += 2)
+                    e = cudaFuncSetAttribute(matvec_kernel(nt, gb, zp, parts), cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem));
     d.clusters[0] = d.sms;
     for (int i = 1; i <= 3 && e == cudaSuccess; i++) {
         cudaLaunchConfig_t cfg{};
@@ -963,7 +990,7 @@ sq_status matvec_device(MatvecDevice *out)
         at.val.clusterDim.y = at.val.clusterDim.z = 1;
         cfg.attrs = &at;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 2, false), &cfg);
+        e = cudaOccupancyMaxActiveClusters(&d.clusters[i], matvec_kernel(1, 2, false, 3), &cfg);
     }
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     g_devices.push_back(d);
@@ -1021,14 +1048,15 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     p.units = int((a.K + kUnitK - 1) / kUnitK);
     p.tiles = int((a.N + kTileN - 1) / kTileN);
 
+    p.parts = p.y_f32 && (p.x_f32 || a.act != SQ_ACT_NONE) ? 5 : 3;
     // Rows of a pass: as many as 32 columns take, spread evenly; fewer where the activations would not fit.
-    const int most = kMaxCols / 3;
+    const int most = kMaxCols / p.parts;
     int passes = (p.M + most - 1) / most;
     double best = 0;
     MatvecParams pick{};
     for (;; passes++) {
         p.rows = (p.M + passes - 1) / passes;
-        p.cols = p.rows * 3;
+        p.cols = p.rows * p.parts;
         p.per_row = 0xFFFFFFFFu / uint32_t(p.rows) + 1u;
         p.cols8 = (p.cols + 7) / 8 * 8;
         for (int ci = 0; ci < 4; ci++) {
@@ -1066,7 +1094,7 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
     cfg.attrs = at;
     cfg.numAttrs = pick.cl > 1 ? 2 : 1;
     void *args[1] = {&pick};
-    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb, p.z != nullptr), args);
+    const cudaError_t e = cudaLaunchKernelExC(&cfg, matvec_kernel(pick.cols8 / 8, gb, p.z != nullptr, p.parts), args);
     if (e != cudaSuccess) { note_cuda_error(e); return SQ_ERR_CUDA; }
     count_launch();
     return SQ_OK;

@@ -1,11 +1,12 @@
 """The matrix-vector product with 4-bit weights at the ends of its ranges: activations that are no numbers behind an activation function,
-zero-points anywhere in int8.
+zero-points anywhere in int8, activations of very different magnitude in front of fp32 outputs.
 
 Tolerances.  u = 2^-24 is a rounding's share.  A term of a sum is on its way through at most 50 + ceil(K / 256) roundings: the zero-point's and the
 scale's multiply-add, up to eight blocks of a unit, the units, then sixteen runs, the bytes, lanes, eight CTAs and the bias.  The bytes that an
 activation is split into are at most 3.03 times as large together as the activation: those below the leading one, 256^p of which the
 activation has at least half of, add up to at most 0.502 of 256^p, and the leading one is off the activation by that much again.
-An activation is off by at most 2^-22 of the largest magnitude of its row in its 256 inputs, or 2^-123.  bf16 outputs are rounded once more, by at
+An activation is off by at most 2^-22 of the largest magnitude of its row in its 256 inputs, or 2^-123; 2^-37 instead of 2^-22 where the output is
+fp32 and the activations are fp32 or come out of an activation function.  bf16 outputs are rounded once more, by at
 most half a step."""
 import pytest
 import torch
@@ -75,3 +76,21 @@ def test_zero_points_of_weights_next_to_nothing():
     X = torch.full((2, 128), float(0x3F7F7F) * 2.0 ** 78, device=DEV)          # (bytes as large as they get)
     for y in (BF, F32):
         check(B.segquant_w4_matvec(X, W4, s_w, 128, z_w, y_dtype=y), X, weights64(W4, s_w, z_w, 128, 128), 128)
+
+
+@pytest.mark.parametrize("ratio", [10.0 ** 3, 10.0 ** 4])
+@pytest.mark.parametrize("act", [None, "silu", "gelu"])
+@pytest.mark.parametrize("M", [1, 2, 5, 13])
+def test_small_activations_beside_a_large_one(M, act, ratio):
+    """fp32 outputs have the digits of fp32 products: one activation in 256 is `ratio` times as large as the other one that there is, and its
+    weights are zero."""
+    K, N, G = 1024, 64, 64
+    W4, s_w, _ = random_codes(N, K, G, False, F32, 13)
+    g = torch.Generator(device=DEV).manual_seed(14)
+    X = torch.zeros((M, K), device=DEV)
+    for u in range(K // 256):
+        X[:, u * 256] = ratio
+        at = torch.randint(1, 256, (M,), generator=g, device=DEV) + u * 256
+        X[torch.arange(M, device=DEV), at] = torch.rand(M, generator=g, device=DEV) + 0.5
+        W4[:, u * 128] &= 0xF0                               # code 0
+    check(B.segquant_w4_matvec(X, W4, s_w, G, act=act, y_dtype=F32), X, weights64(W4, s_w, None, G, K), K, act, fixed=2.0 ** -37)
