@@ -308,8 +308,8 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     ldz; groups = ceil(K / group), the last one may be short.  group: 32, 64, 128 or a multiple of 256.
  *   segquant_dequantize_w4_group: W [N,K] of dtype dt from them, one fp32 product each, rounded once to dt.
  *   segquant_w4_matvec: y[m][n] = sum_g s[g][n] * ( sum_{k in g} (c[n][k] - z[g][n]) * a[m][k] ) + bias[n],
- *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused; NOT rounded
- *     to dt in between).  a enters as a fixed-point number, off by at most 2^-22 of the largest |a| among the 256 inputs
+ *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused, with
+ *     y_dtype fp32 a relative 2^-20 for values that are no subnormals; NOT rounded to dt in between).  a enters as a fixed-point number, off by at most 2^-22 of the largest |a| among the 256 inputs
  *     k / 256 of its row (or 2^-123); bf16 values down to 2^-14 of that largest one are exact.  With y_dtype fp32, and X fp32 or an act, by at most
  *     2^-37 of it (or 2^-123), so that such outputs have the digits of fp32 products; fp32 values down to 2^-13 of the largest are exact.  Sums over a group (128 inputs of a
  *     longer one) are exact (rounded once where a zero-point is outside [-8, 7]), the rest is fp32 in an order that depends on the sizes and the device alone; one

@@ -719,12 +719,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
                 if (++b == kAhead) b = 0, fetch();
                 if (prm.act == SQ_ACT_SILU) {
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) unpack2(silu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                    for (int j = 0; j < 8; j += 2) {
+                        if constexpr (PARTS == 5) x[j] = silu_precise(x[j]), x[j + 1] = silu_precise(x[j + 1]);
+                        else unpack2(silu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                    }
                 } else if (prm.act == SQ_ACT_GELU) {
                     const float in = largest8(x);
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) unpack2(gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
-                    if (!(in < __uint_as_float(0x7F800000u))) x[0] = in;                // (it makes 0 of a NaN and of -infinity)
+                    for (int j = 0; j < 8; j += 2) {
+                        if constexpr (PARTS == 5) x[j] = gelu_precise(x[j]), x[j + 1] = gelu_precise(x[j + 1]);
+                        else unpack2(gelu2(x[j], x[j + 1]), x[j], x[j + 1]);
+                    }
+                    if (!(in < __uint_as_float(0x7F800000u))) x[0] = in;                // (GELU may make 0 of a NaN and of -infinity)
                 }
                 float top = largest8(x);
 #pragma unroll

@@ -94,3 +94,24 @@ def test_small_activations_beside_a_large_one(M, act, ratio):
         X[torch.arange(M, device=DEV), at] = torch.rand(M, generator=g, device=DEV) + 0.5
         W4[:, u * 128] &= 0xF0                               # code 0
     check(B.segquant_w4_matvec(X, W4, s_w, G, act=act, y_dtype=F32), X, weights64(W4, s_w, None, G, K), K, act, fixed=2.0 ** -37)
+
+
+@pytest.mark.parametrize("x", [BF, F32])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_activation_functions_in_front_of_fp32_outputs(x, act):
+    """One activation a row, over the range in which its function's value is an ordinary number: 16 roundings and the bytes' own (a number's
+    bytes below the leading one, which is at least 32 here, are together at most 0.502 / 32 of it, so that all but the last of their
+    additions round 2^-24 of less than a sixtieth)."""
+    K, N, G, M = 32, 8, 32, 8192
+    W4 = torch.zeros((N, 16), dtype=torch.uint8, device=DEV)
+    W4[:, 3] = 0x01                                          # input 6 alone counts, once
+    s_w = torch.ones((1, N), device=DEV)
+    X = torch.zeros((M, K), device=DEV, dtype=x)
+    X[:, 6] = torch.linspace(-80.0 if act == "silu" else -9.0, 9.0, M, device=DEV).to(x)
+    Y = B.segquant_w4_matvec(X, W4, s_w, G, act=act, y_dtype=F32)
+    v = X[:, 6].double()
+    want = act64(v, act)
+    tol = want.abs() * (16 * U + 2.0 ** -37 + 1.1 * U) + 2.0 ** -123
+    err = (Y[:, 0].double() - want).abs()
+    assert bool(torch.all(err <= tol)), f"worst {float((err / tol).max()):.3g} of the tolerance"
+    assert torch.equal(Y, Y[:, :1].expand(M, N))
