@@ -315,7 +315,8 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     longer one) are exact (rounded once where a zero-point is outside [-8, 7]), the rest is fp32 in an order that depends on the sizes and the device alone; one
  *     rounding to y_dtype.  A row with an infinity or a NaN in X has NaN for outputs, whatever act makes of it.  X [M,K] dev (dtype dt, ldx
  *     elements), bias dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements
- *     only; Y must not overlap X, bias, Wq4, s_w or z_w.  Codes of any 4 bits, any zero-points.  K <= 131072, M <= 65535,
+ *     only; Y must not overlap X, bias, Wq4, s_w or z_w.  Codes of any 4 bits, any zero-points, |s_w| up to 2^96 (a scale
+ *     meets whole numbers of up to 2^28 before the activations' exponent; larger ones may overflow there).  K <= 131072, M <= 65535,
  *     meant for M of at most about 32 (the weights are read once per pass of up to 10 rows, 6 where 2^-37 holds).  No workspace.
  *   The quantizer's outputs must not overlap W or one another, the dequantizer's W not Wq4, s_w or z_w (SQ_ERR_UNSUPPORTED).
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.

@@ -115,3 +115,21 @@ def test_activation_functions_in_front_of_fp32_outputs(x, act):
     err = (Y[:, 0].double() - want).abs()
     assert bool(torch.all(err <= tol)), f"worst {float((err / tol).max()):.3g} of the tolerance"
     assert torch.equal(Y, Y[:, :1].expand(M, N))
+
+
+@pytest.mark.parametrize("x,y", [(BF, F32), (F32, F32), (F32, BF)])
+def test_scales_up_to_2_96(x, y):
+    K, N, G = 512, 40, 32
+    W4, s_w, _ = random_codes(N, K, G, False, F32, 15)
+    z_w = torch.randint(-128, 128, (K // G, 48), device=DEV, dtype=torch.int8)[:, :N]
+    s_w.copy_(s_w.clone().clamp(0.008, 0.01) * (2.0 ** 96 / 0.01))
+    X = (torch.randn((3, K), device=DEV) * 2.0 ** -60).to(x)
+    check(B.segquant_w4_matvec(X, W4, s_w, G, z_w, y_dtype=y), X, weights64(W4, s_w, z_w, G, K), K)
+
+
+@pytest.mark.parametrize("x,y", [(BF, BF), (F32, F32)])
+@pytest.mark.parametrize("M,K,N,G", [(1, 2000, 33, 768), (4, 3000, 50, 768), (2, 2700, 24, 1280), (3, 700, 17, 768)])
+def test_groups_that_are_no_power_of_two(M, K, N, G, x, y):
+    W4, s_w, z_w = random_codes(N, K, G, True, F32, 16)
+    X = torch.randn((M, K), device=DEV).to(x)
+    check(B.segquant_w4_matvec(X, W4, s_w, G, z_w, y_dtype=y), X, weights64(W4, s_w, z_w, G, K), K)
