@@ -345,7 +345,8 @@ sq_status segquant_w4_matvec(const void *X, sq_dtype dt, int64_t M, int64_t K, i
  *     where the exact quotient lies that close to a rounding boundary.
  *   Y, R, H, O dev, dtype dt, pitches in elements; H and O may be Y or R themselves (same address and pitch), any other overlap
  *   of an output with an input, a vector, the scales or another output is refused with SQ_ERR_UNSUPPORTED.  Alignment: Y, R, H, O and codes 16 bytes, pitches multiples of 16 bytes; the vectors
- *   that of their elements.  C <= 16384.  Values beyond about 2^60 overflow the sums of squares. */
+ *   that of their elements.  C <= 16384.  Values (centred ones for a layer norm) of
+ *   2^64 / sqrt(C) and more overflow the sums of squares: 2^57 at C = 16384. */
 typedef enum { SQ_NORM_NONE = 0, SQ_NORM_RMS = 1, SQ_NORM_LAYER = 2 } sq_norm;
 typedef struct {
     sq_norm post;                             /* norm of the block's output */
