@@ -24,6 +24,7 @@ class SegQuantLinear:
         self.bias = None if bias is None else bias.to(self.device, torch.float32).contiguous()
         self.s_pos = self.s_neg = None
         self._scratch = None
+        self._outgrown = []              # buffers that captured calls may still refer to
 
     def calibrate(self, X_cal: torch.Tensor):
         """Min/max activation scales from a calibration batch (offline)."""
@@ -38,8 +39,14 @@ class SegQuantLinear:
         self.workspace = B.new_workspace(self.device, split_for=(M, self.N, self.dual))
 
     def scratch_for(self, M: int) -> torch.Tensor:
+        """The codes of an input of M rows.  The layer's calls share it: calls that may run at once (other streams) need a layer object
+        each.  A buffer that has been handed out stays as long as the layer does, because a CUDA graph keeps its address; every new
+        one is at least twice as large as the last, so that those kept are together no larger than the one in use."""
         need = B.layer_scratch_bytes(M, self.K, self.dual)
         if self._scratch is None or self._scratch.numel() < need:
+            if self._scratch is not None:
+                self._outgrown.append(self._scratch)
+                need = max(need, 2 * self._scratch.numel())
             self._scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._scratch
 
