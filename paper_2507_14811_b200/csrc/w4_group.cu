@@ -1072,14 +1072,15 @@ sq_status launch_w4_matvec(const W4MatvecArgs &a, cudaStream_t st)
             p.clusters = std::min(p.tiles, dev.clusters[ci]);
             const int tiles = (p.tiles + p.clusters - 1) / p.clusters;
             if (!lay_out(p, gb, tiles)) continue;
-            // Microseconds, fitted to cl = 1, 2 and 4 forced on 16 shapes: a CTA's units (more columns and shorter groups take
+            // Microseconds, fitted to cl = 1, 2, 4 and 8 forced on 31 shapes: a CTA's units (more columns and shorter groups take
             // more instructions, a shallow ring waits more), converting its activations, its outputs, a cluster's
-            // barriers, and starting over where the tiles' sums do not fit at once.
+            // barriers, and starting over where the tiles' sums do not fit at once.  (The fastest of the four is missed by at most
+            // 3 % on 30 of them, 9 % on the other: 6 x 4608 -> 18432 fp32, 29.4 against 27.1 us.)
             const int nt = p.cols8 / 8;
             const double unit = 0.035 + 0.02 * nt + (gb == 8 ? 0.02 : gb == 4 ? 0.007 : 0.0) * nt;
             const double cost = unit * (1.0 + 0.1 * (kMaxStages - p.stages)) * tiles * p.units_cta +
-                                (p.act != SQ_ACT_NONE ? 0.05 : 0.035) * p.rows * p.units_cta +
-                                0.4 * ((tiles * kTileN * p.rows + kWarps * 32 - 1) / (kWarps * 32)) + (ci ? 0.9 : 0.0) +
+                                (p.act != SQ_ACT_NONE ? 0.05 : 0.035) * (p.parts == 5 ? 1.8 : 1.0) * p.rows * p.units_cta +
+                                0.4 * ((tiles * kTileN * p.rows + kWarps * 32 - 1) / (kWarps * 32)) + (ci ? 0.7 + 0.2 * ci : 0.0) +
                                 8.0 * ((tiles + p.tiles_round - 1) / p.tiles_round - 1);
             if (best == 0 || cost < best) best = cost, pick = p;
         }
