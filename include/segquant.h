@@ -308,16 +308,17 @@ sq_status segquant_w4a8_gemm(const void *Xq_pos, const void *Xq_neg, int64_t ldx
  *     ldz; groups = ceil(K / group), the last one may be short.  group: 32, 64, 128 or a multiple of 256.
  *   segquant_dequantize_w4_group: W [N,K] of dtype dt from them, one fp32 product each, rounded once to dt.
  *   segquant_w4_matvec: y[m][n] = sum_g s[g][n] * ( sum_{k in g} (c[n][k] - z[g][n]) * a[m][k] ) + bias[n],
- *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused, with
- *     y_dtype fp32 a relative 2^-20 for values that are no subnormals; NOT rounded to dt in between).  a enters as a fixed-point number, off by at most 2^-22 of the largest |a| among the 256 inputs
- *     k / 256 of its row (or 2^-123); bf16 values down to 2^-14 of that largest one are exact.  With y_dtype fp32, and X fp32 or an act, by at most
- *     2^-37 of it (or 2^-123), so that such outputs have the digits of fp32 products; fp32 values down to 2^-13 of the largest are exact.  Sums over a group (128 inputs of a
- *     longer one) are exact (rounded once where a zero-point is outside [-8, 7]), the rest is fp32 in an order that depends on the sizes and the device alone; one
- *     rounding to y_dtype.  A row with an infinity or a NaN in X has NaN for outputs, whatever act makes of it.  X [M,K] dev (dtype dt, ldx
- *     elements), bias dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements
- *     only; Y must not overlap X, bias, Wq4, s_w or z_w.  Codes of any 4 bits, any zero-points, |s_w| up to 2^96 (a scale
- *     meets whole numbers of up to 2^28 before the activations' exponent; larger ones may overflow there).  K <= 131072, M <= 65535,
- *     meant for M of at most about 32 (the weights are read once per pass of up to 10 rows, 6 where 2^-37 holds).  No workspace.
+ *     a = x, or with act SQ_ACT_SILU / SQ_ACT_GELU the activation of x (accuracy as for segquant_quantize_act_fused, with y_dtype
+ *     fp32 a relative 2^-20 for values that are no subnormals; NOT rounded to dt in between).  a enters as a fixed-point number, off by
+ *     at most 2^-22 of the largest |a| among the 256 inputs k / 256 of its row (or 2^-123); bf16 values down to 2^-14 of that largest
+ *     one are exact.  With y_dtype fp32, and X fp32 or an act, by at most 2^-37 of it (or 2^-123), so that such outputs have the
+ *     digits of fp32 products; fp32 values down to 2^-13 of the largest are exact.  Sums over a group (128 inputs of a longer one) are exact (rounded once where a zero-point is outside
+ *     [-8, 7]), the rest is fp32 in an order that depends on the sizes and the device alone; one rounding to y_dtype.
+ *     A row with an infinity or a NaN in X has NaN for outputs, whatever act makes of it.  X [M,K] dev (dtype dt, ldx elements), bias
+ *     dev [N] fp32 or NULL, Y [M,N] dev of y_dtype, ldy elements; X, bias and Y need the alignment of their elements only; Y must
+ *     not overlap X, bias, Wq4, s_w or z_w.  Codes of any 4 bits, any zero-points, |s_w| up to 2^96 (a scale meets whole numbers of up
+ *     to 2^28 before the activations' exponent; larger ones may overflow there).  K <= 131072, M <= 65535, meant for M of at most
+ *     about 32 (the weights are read once per pass of up to 10 rows, 6 where 2^-37 holds).  No workspace.
  *   The quantizer's outputs must not overlap W or one another, the dequantizer's W not Wq4, s_w or z_w (SQ_ERR_UNSUPPORTED).
  *   Alignment: W, Wq4, s_w, z_w 16 bytes; ld*sizeof(dt), ldw, lds*sizeof(s_dtype), ldz multiples of 16 bytes.
  *     N <= 4194240 for segquant_dequantize_w4_group. */

@@ -393,7 +393,8 @@ _W4_ACT = {None: 0, "none": 0, "silu": 1, "gelu": 2}
 
 def segquant_w4_matvec(X: torch.Tensor, Wq4, s_w, group: int, z_w=None, bias=None, act=None, y_dtype=torch.bfloat16, Y=None):
     """Few rows X [M, K] times the transpose of 4-bit weights with group scales, the activation function in front and the
-    bias behind: Y [M, N].  Weights as segquant_quantize_w4_group makes them."""
+    bias behind: Y [M, N].  Weights as segquant_quantize_w4_group makes them; zero-points may be any int8.  fp32 outputs of fp32 or activated inputs
+    have the digits of fp32 products (and take longer for more than one row)."""
     st, Y = _calls().w4_matvec(X, Wq4, s_w, group, z_w, bias, _named(_W4_ACT, act, "activation"), Y, _real(y_dtype))
     _check(st, "segquant_w4_matvec")
     return Y

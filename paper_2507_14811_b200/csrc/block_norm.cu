@@ -562,7 +562,9 @@ __global__ void __launch_bounds__(WPR * RPB * L, BLOCKS) block_norm_kernel(const
 }
 
 // One shape: CH chunks a lane, WPR warps per row, RPB rows of a block at a time.  A warp per row up to 1280 bf16 (1024 fp32) channels
-// where there are at least five per SM, two, four and eight up to 8192, then a block per row; fewer rows get a block each.  (2048 x 5120:
+// where there are at least five per SM, two, four and eight up to 8192, then a block per row; fewer rows get a block each: of two and more per SM several share an SM, so
+// blocks are small (300 x 12000 14.2 us against 20.7 with blocks as wide as below, 700 x 16384 29.0 against 40.1, 600 x 4096 8.6 against 9.6; 600 x 1536
+// 6.2 against 5.7, 400 x 8192 11.9 against 10.6), below that as many warps as a row keeps busy (160 x 1536 3.5 us against 4.7, 290 x 8192 8.0 against 9.0).  (2048 x 5120:
 // 35 us with a block per row, 20.5 with two rows a block, which share their vectors.)  Rows of up to 128
 // channels take 8 or 16 lanes (32768 x 64: 14.1 -> 5.5 us).  Samples of fewer than 16 rows: every row makes its vectors (16384 x 640, a vector
 // per row: 93.7 us with a block per row, 51.4 with a warp).  (8858 x 1536 bf16 to codes: one warp with six chunks a lane, held to 128 registers, 28.1 us; two with three

@@ -342,7 +342,8 @@ float *f32_vector(const Args &a, int i, int64_t n, const char *what)
 }
 
 // [rows, cols] on the device of a CUDA tensor, with rows on boundaries of `unit` elements.  Past the dispatcher and without a view: half
-// the time of at::empty and narrow (a call with one output of an odd width 5.9 -> 4.6 us).
+// the time of at::empty and narrow (a call with one output of an odd width 5.9 -> 4.6 us).  The price: torch's modes that watch
+// new tensors or fill them do not see these.
 at::Tensor new_rows(int64_t rows, int64_t cols, const at::Tensor &like, at::ScalarType type, int64_t unit = 16)
 {
     on_device(like, "a tensor");

@@ -7,7 +7,8 @@
 // instructions per code, and half of that on either arithmetic pipe, so codes are not turned into real numbers one by one.  A byte of
 // two codes is two signed bytes 16 c after one mask each (0.4 instructions per code), which integer matrix instructions take as they are:
 // mma.m16n8k32, 16 channels on its rows.  The activations become 23-bit fixed-point numbers, as three signed bytes in three of
-// its 8 columns (38 bits in five, where fp32 activations make fp32 outputs); products and a group's sums are exact integers, and scales and zero-points come in behind a group.
+// its 8 columns (38 bits in five, where fp32 activations make fp32 outputs); products and a group's sums are exact integers, and
+// scales and zero-points come in behind a group.
 // (Expanded to bf16 instead, 1.4 instructions per code, the same design took 38.3 us for 1 x 8192 -> 28672 with zero-points.)  tcgen05
 // would want the expanded codes in shared memory, twice the bytes that came in, and has nothing to offer: the tensor pipe is no bound here.
 #include <cuda_bf16.h>
@@ -550,15 +551,18 @@ __device__ __forceinline__ int lanes_of_output(int tiles, int outs)
 // of K will do as long as both operands have it.
 //
 // Fixed point: with 2^E <= max|x| < 2^(E+1) over the 256 inputs of a unit, q = round(x 2^(21 - E)), |q| <= 2^22, off by at most
-// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact, and behind a bf16 rounding of the outputs the others are good enough); the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2
-// with q = q0 + 256 q1 + 65536 q2.  fp32 outputs of fp32 activations, or of an activation function's values, are to have the digits of fp32
-// products: round(2^15 (x 2^(21 - E) - q)) follows in two more bytes, off by at most 2^-37 of the maximum (an fp32 x down to 2^-13 of it
-// is exact).  The rule looks at types alone.  (Three bytes there: an input in 256 a thousand times the others, weights of theirs
-// a thousand times its own: 4.9e-5 of the output instead of 2e-7.)  A block, a group or 128 inputs of a longer one, has a sum of 16 c q_i within 2^21, so that it becomes
-// a float by starting at the bits of 1.5 * 2^23, the MMA's addend, and subtracting that number.  One FMA takes off the zero-point times the
-// block's sum of 16 q_i (both are whole numbers of fp32; their product and the difference are, too, for zero-points in [-8, 7], and are rounded
-// once beyond; as the MMA's addend they would leave the range of the start for those).  One FMA takes it with its scale to the unit's sum, and one
-// the unit's sum with 2^(E - 25) 256^i to the tile's.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
+// 2^-22 of that maximum (a bf16 x down to 2^-14 of it is exact, and behind a bf16 rounding of the outputs the others are good enough);
+// the lower three bytes of (q + 0x8080) ^ 0x8080 are signed q0, q1, q2 with q = q0 + 256 q1 + 65536 q2.
+// fp32 outputs of fp32 activations, or of an activation function's values, are to have the digits of fp32 products: there
+// round(2^15 (x 2^(21 - E) - q)) makes two more bytes, off by at most 2^-37 of the maximum (an fp32 x down to 2^-13 of it is exact).
+// The rule looks at types alone.  (Three bytes there: an input in 256 a thousand times the others, its weights a thousand times
+// smaller: 4.9e-5 of the output instead of 2e-7.  Five cost a row nothing, 25.9 -> 26.0 us for 1 x 8192 -> 28672, two rows 26.7 -> 33.0;
+// 8 x 4608 -> 18432 19.3 -> 41.3, because more than six take a second pass.)
+// A block, a group or 128 inputs of a longer one, has a sum of 16 c q_i within 2^21, so that it becomes a float by starting at the
+// bits of 1.5 * 2^23, the MMA's addend, and subtracting that number.  One FMA takes off the zero-point times the block's sum of 16 q_i
+// (whole numbers of fp32, as are their product and the difference for zero-points in [-8, 7]; beyond, one rounding.  As the MMA's addend
+// they would leave the range of the start there).  One FMA takes it with its scale to the unit's sum, and one the unit's sum with
+// 2^(E - 25) 256^i to the tile's, two columns per instruction.  A unit with an infinity or a NaN has the factor NaN.  (A range per group
 // instead of one per unit: 26.3 us against 25.8 for 1 x 8192 -> 28672, 9.7 against 8.8 for 8 x 1536 -> 9216 with SiLU.)
 // GB: blocks of a unit (2, 4, 8).  PARTS: bytes of an activation (3, 5).
 template <int NT, int GB, bool ZP, int PARTS>
@@ -736,10 +740,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_matvec_kernel(const __grid_
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                 const bool finite = top < __uint_as_float(0x7F800000u);
-                const uint32_t be = max(__float_as_uint(top) >> 23, PARTS == 5 ? 41u : 26u);     // biased E; smaller ranges count as 2^-86, 2^-101
+                // biased E; smaller ranges count as 2^-86 (five bytes) and 2^-101
+                const uint32_t be = max(__float_as_uint(top) >> 23, PARTS == 5 ? 41u : 26u);
                 const float up = finite ? __uint_as_float((275u - be) << 23) : 0.0f;    // 2^(21 - E); (other blocks: any bytes)
                 uint8_t *dst = smem + prm.x_off + size_t(e >> 3) * x_pair + (e & 3) * 16 + (e >> 2 & 1) * 8;
-                // the lower COUNT bytes of v, the uppermost as it is if it is the number's own, to columns p, p + 1, ..
+                // the lower COUNT bytes of v to columns p0, p0 + 1, ..: the first two offset by 128, a third signed as it is
                 auto put = [&](const uint32_t (&v)[8], int p0, auto count) {
                     constexpr int COUNT = decltype(count)::value;
                     uint32_t even[3], odd[3];

@@ -109,7 +109,9 @@ class SegQuantLinear:
 
 class W4GroupLinear:
     """Linear layer for few rows with 4-bit weights, one scale (and zero-point) per output channel and group of inputs; the
-    activations stay real numbers.  The modulation projection of a block (one conditioning vector per sample), single tokens."""
+    activations stay real numbers.  The modulation projection of a block (one conditioning vector per sample), single tokens.  Any number of
+    rows is taken, but the weights are read again for every 10 of them (6 with fp32 outputs of fp32 or activated inputs): from about 12 rows on
+    small layers and 32 on large ones a library product on `weights()` takes less time, those made anew each time included."""
 
     def __init__(self, W: torch.Tensor, bias=None, group: int = 128, zero_points: bool = False, s_dtype=torch.float32, device="cuda"):
         self.device = torch.device(device)
